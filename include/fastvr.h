@@ -283,6 +283,118 @@ fastvr_status fastvr_tile_blend_update(const float* v_tiles, const void* z_lq, f
                                        int64_t T, int64_t Hg, int64_t Wg, int64_t C, int64_t tile, int64_t overlap,
                                        void* stream);
 
+/*
+ * Rotary positions of query or key heads, and their gradient.  In each head the
+ * first 2 * n_pairs elements are n_pairs points of the plane, the others pass
+ * unchanged.  Pair p turns by the angle position[axis(p)] * inv_freq[p]:
+ *   (a, b)  ->  amplitude * (a cos - b sin, a sin + b cos)
+ * with (a, b) = elements (2p, 2p + 1) when interleaved, (p, p + n_pairs)
+ * otherwise.  inverse = 1 turns by the negative angle, with the same amplitude: the
+ * gradient of the call with inverse = 0.  Angles are taken in fp64 (positions up
+ * to 2^31 keep their fraction of a turn), the products in fp32.
+ *
+ *   x          bf16 (x_fp32 = 0) or fp32 [B, N, H, d] view   input
+ *   y          bf16 (y_fp32 = 0) or fp32 [B, N, H, d] view   output, fully overwritten
+ *   positions  int32 [B, N, n_axes] (batch stride pos_sb, 0: shared)   position of each token
+ *   inv_freq   fp64 [n_pairs]                                radians per position
+ * Pairs p < split1 turn with axis 0, split1 <= p < split2 with axis 1, the others
+ * with axis 2 (a frame, row and column of a video token, say); axes that do not
+ * exist own no pairs: split1 = n_pairs for one axis, split2 = n_pairs for two.
+ *
+ * Preconditions (else FASTVR_ERR_INVALID_ARGUMENT unless noted): sizes >= 0; d in
+ * {64, 128}, B <= 65535 and N * H * d < 2^33 (else FASTVR_ERR_UNSUPPORTED);
+ * 0 <= n_pairs <= d / 2; 1 <= n_axes <= 3; 0 <= split1 <= split2 <= n_pairs as above;
+ * view rules of fastvr_chunk_attn_fwd_ex for x and y; positions 4-byte and
+ * inv_freq 8-byte aligned, non-NULL (inv_freq may be NULL when n_pairs = 0);
+ * pos_sb = 0 or >= N * n_axes; amplitude finite; y overlaps no input, except that
+ * it may be exactly x (same pointer, type and strides): in place.
+ * B, N or H equal to 0: FASTVR_OK, nothing enqueued.
+ */
+fastvr_status fastvr_rope(const void* x, int64_t x_sb, int64_t x_st, int32_t x_fp32, void* y, int64_t y_sb,
+                          int64_t y_st, int32_t y_fp32, const int32_t* positions, int64_t pos_sb, int64_t n_axes,
+                          int64_t split1, int64_t split2, const double* inv_freq, int64_t n_pairs, double amplitude,
+                          int32_t interleaved, int32_t inverse, int64_t B, int64_t N, int64_t H, int64_t d,
+                          void* stream);
+
+/*
+ * KV cache in 4 bits: microscaled e2m1 elements (values 0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * and their negatives) with one power-of-two scale for 32 elements along head_dim,
+ * 0.53 instead of 2 bytes an element.  The cache is four tensors, head by head
+ * (a head's tokens are contiguous):
+ *   k_codes,  v_codes   uint8 [B, H, capacity, d / 2]    element 2i in the low half of byte i
+ *   k_scales, v_scales  uint8 [B, H, capacity, d / 32]   scale 2^(byte - 127), 2 <= byte <= 252; 255: NaN
+ * A block's scale 2^e is the one that puts its largest magnitude a into
+ * [3.5, 7) 2^e (-125 <= e <= 125), so that a goes to the nearest of 4 2^e and 6 2^e;
+ * each element goes to the nearest value, ties to the even code.  A block that holds an
+ * infinity or NaN stands for NaN (byte 255, codes 0).  The values that codes and
+ * scales stand for are exact in bf16.
+ *
+ * fastvr_kv4_append: n_new rows of K and V (bf16 [B, n_new, H, d] views) go to
+ * token rows first .. first + n_new - 1 of every sequence, or, when starts (int32
+ * [B], device memory) is given, to rows starts[b] + 0 .. n_new - 1 of sequence b
+ * (first is not used then); of these, rows outside 0 .. capacity - 1 are dropped.
+ * All other rows are left as they are.
+ * fastvr_kv4_read: the values of n token rows, first or starts as above, as bf16
+ * [B, n, H, d] views; with starts, rows outside the cache read as zero.
+ *
+ * Preconditions (else FASTVR_ERR_INVALID_ARGUMENT unless noted): sizes >= 0; d in
+ * {64, 128}, B <= 32767, H <= 65535, capacity <= FASTVR_KV4_MAX_CAPACITY (else
+ * FASTVR_ERR_UNSUPPORTED); without starts, first >= 0 and first + n <= capacity
+ * (else FASTVR_ERR_CAPACITY); cache tensors contiguous, 16-byte aligned, and
+ * overlapping nothing; view rules of fastvr_chunk_attn_fwd_ex for the bf16 tensors;
+ * outputs overlap nothing; starts NULL or 4-byte aligned.
+ * B, H, n_new or n equal to 0: FASTVR_OK, nothing enqueued.
+ */
+#define FASTVR_KV4_MAX_CAPACITY (16 * 1024 * 1024)
+fastvr_status fastvr_kv4_append(void* k_codes, void* k_scales, void* v_codes, void* v_scales, const void* k_new,
+                                int64_t k_sb, int64_t k_st, const void* v_new, int64_t v_sb, int64_t v_st,
+                                const int32_t* starts, int64_t B, int64_t H, int64_t d, int64_t capacity,
+                                int64_t first, int64_t n_new, void* stream);
+fastvr_status fastvr_kv4_read(const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales,
+                              void* k_out, int64_t k_sb, int64_t k_st, void* v_out, int64_t v_sb, int64_t v_st,
+                              const int32_t* starts, int64_t B, int64_t H, int64_t d, int64_t capacity, int64_t first,
+                              int64_t n, void* stream);
+
+/*
+ * Chunk-causal attention of the newest tokens over a 4-bit cache: from one token
+ * of each sequence (serving) to whole chunks (streaming).  Sequence b holds
+ * len_b = cache_len tokens or, when lens (int32 [B], device memory) is given,
+ * len_b = min(max(lens[b], 0), cache_len).  Query row i is the token at position
+ * P = len_b - Nq + i, which lies in chunk c = P / chunk_len and sees the keys
+ *   max(0, c - window_chunks) * chunk_len .. min((c + 1) * chunk_len, len_b) - 1
+ * (window_chunks = -1: from 0).  chunk_len >= cache_len: every row sees the whole
+ * cache; chunk_len = 1: token-causal, window_chunks = w - 1 a sliding window of w
+ * tokens.  Rows with P < 0 (padding in front of a short sequence) see nothing:
+ * O = 0 and LSE = -infinity.  H query heads share Hkv key heads in order:
+ * query head h reads key head h / (H / Hkv).  A key that a row does not see has no
+ * effect on it, whatever it stands for.
+ *
+ *   q    bf16 [B, Nq, H, d] view
+ *   o    fp32 (o_bf16 = 0) or bf16 [B, Nq, H, d] view, fully overwritten
+ *   lse  fp32 [B, H, Nq] contiguous, or NULL
+ *   workspace  16-byte aligned device memory of workspace_bytes >= what
+ *              fastvr_kv4_attn_workspace gives for these sizes (may be NULL for 0);
+ *              the call's own until its work on `stream` has ended
+ * Results do not depend on the workspace's contents; equal calls give equal bits.
+ *
+ * Preconditions (else FASTVR_ERR_INVALID_ARGUMENT unless noted): sizes >= 0; d in
+ * {64, 128}; H a multiple of Hkv; 0 <= cache_len <= capacity; chunk_len >= 1;
+ * window_chunks >= -1; scale finite; cache tensors contiguous, 16-byte aligned; view
+ * rules of fastvr_chunk_attn_fwd_ex for q and o; lens NULL or 4-byte aligned; o,
+ * lse and workspace overlap nothing; capacity <= FASTVR_KV4_MAX_CAPACITY, Nq * H
+ * and token strides below 2^31 and not more work items than one launch holds (else
+ * FASTVR_ERR_UNSUPPORTED).
+ * B, H or Nq equal to 0: FASTVR_OK, nothing enqueued.
+ */
+fastvr_status fastvr_kv4_attn_workspace(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d, int64_t cache_len,
+                                        int64_t chunk_len, int64_t window_chunks, int64_t* bytes);
+fastvr_status fastvr_kv4_attn(const void* q, int64_t q_sb, int64_t q_st, const void* k_codes, const void* k_scales,
+                              const void* v_codes, const void* v_scales, void* o, int64_t o_sb, int64_t o_st,
+                              int32_t o_bf16, float* lse, void* workspace, int64_t workspace_bytes,
+                              const int32_t* lens, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d,
+                              int64_t capacity, int64_t cache_len, int64_t chunk_len, int64_t window_chunks,
+                              float scale, void* stream);
+
 /* Static string naming a status code ("FASTVR_OK", ...); never NULL. */
 const char* fastvr_status_string(fastvr_status s);
 

@@ -11,6 +11,7 @@
 #include <cstdio>
 #include <string>
 
+#include "kv4_plan.h"
 #include "launch.h"
 
 namespace {
@@ -561,6 +562,310 @@ fastvr_status fastvr_tile_blend_update(const float* v_tiles, const void* z_lq, f
   if (z_lq == nullptr && B > 0 && T > 0 && Hg > 0 && Wg > 0 && C > 0)
     return fail(FASTVR_ERR_INVALID_ARGUMENT, "z_lq is NULL");
   return blend_impl(v_tiles, z_lq, z_hat, sigma, B, T, Hg, Wg, C, tile, tile_overlap, stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+// The four tensors of a 4-bit cache: [B, H, capacity, d / 2] codes and
+// [B, H, capacity, d / 32] scales, for K and V.
+struct Kv4Tensors {
+  const void* ptr[4];
+  int64_t bytes[4];
+};
+const char* const kKv4Names[4] = {"k_codes", "k_scales", "v_codes", "v_scales"};
+
+fastvr_status check_kv4(const void* kc, const void* ks, const void* vc, const void* vs, int64_t B, int64_t H,
+                        int64_t d, int64_t capacity, Kv4Tensors* t) {
+  *t = Kv4Tensors{{kc, ks, vc, vs}, {0, 0, 0, 0}};
+  int64_t rows;
+  if (!mul_ok(B, H, &rows) || !mul_ok(rows, capacity, &rows))
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "cache size overflows int64");
+  for (int i = 0; i < 4; ++i) {
+    if (!mul_ok(rows, i % 2 == 0 ? d / 2 : d / 32, &t->bytes[i]))
+      return fail(FASTVR_ERR_INVALID_ARGUMENT, "cache size overflows int64");
+    if (t->bytes[i] == 0) continue;  // a cache without rows
+    if (t->ptr[i] == nullptr) return fail(FASTVR_ERR_INVALID_ARGUMENT, "%s is NULL", kKv4Names[i]);
+    if (!aligned(t->ptr[i], 16)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "%s is not 16-byte aligned", kKv4Names[i]);
+  }
+  return FASTVR_OK;
+}
+
+// Index of the first cache tensor that overlaps the n bytes at p, or -1.
+int kv4_overlap(const Kv4Tensors& t, const void* p, int64_t n) {
+  for (int i = 0; i < 4; ++i)
+    if (n > 0 && t.bytes[i] > 0 && overlap(t.ptr[i], t.bytes[i], p, n)) return i;
+  return -1;
+}
+
+fastvr_status no_kernels(const char* what) {
+  return fail(FASTVR_ERR_HIP, "%s: this build has no kernels", what);
+}
+
+// Append (write = true: k, v are read, the cache is written) or read back.
+fastvr_status kv4_copy(bool write, const void* kc, const void* ks, const void* vc, const void* vs, const void* k,
+                       int64_t k_sb, int64_t k_st, const void* v, int64_t v_sb, int64_t v_st, const int32_t* starts,
+                       int64_t B, int64_t H, int64_t d, int64_t capacity, int64_t first, int64_t n, void* stream) {
+  const char* const names[2] = {write ? "k_new" : "k_out", write ? "v_new" : "v_out"};
+  if (B < 0 || H < 0 || capacity < 0 || n < 0)
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "negative size (B=%lld H=%lld capacity=%lld n=%lld)", (long long)B,
+                (long long)H, (long long)capacity, (long long)n);
+  if (d != 64 && d != 128) return fail(FASTVR_ERR_UNSUPPORTED, "head_dim %lld not in {64, 128}", (long long)d);
+  if (capacity > FASTVR_KV4_MAX_CAPACITY)
+    return fail(FASTVR_ERR_UNSUPPORTED, "capacity %lld > %lld", (long long)capacity,
+                (long long)FASTVR_KV4_MAX_CAPACITY);
+  if (starts == nullptr) {
+    int64_t end;
+    if (first < 0) return fail(FASTVR_ERR_INVALID_ARGUMENT, "first = %lld < 0", (long long)first);
+    if (!add_ok(first, n, &end) || end > capacity)
+      return fail(FASTVR_ERR_CAPACITY, "first + n = %lld + %lld > capacity = %lld", (long long)first, (long long)n,
+                  (long long)capacity);
+  } else if (!aligned(starts, 4)) {
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "starts is not 4-byte aligned");
+  }
+  if (B == 0 || H == 0 || n == 0) return ok();
+  if (B > 32767 || H > 65535) return fail(FASTVR_ERR_UNSUPPORTED, "B > 32767 or H > 65535");
+  if (n > INT32_MAX) return fail(FASTVR_ERR_UNSUPPORTED, "n must be below 2^31");
+  Kv4Tensors t;
+  fastvr_status s = check_kv4(kc, ks, vc, vs, B, H, d, capacity, &t);
+  if (s != FASTVR_OK) return s;
+  const int64_t hd = H * d;
+  int64_t kb, vb, sb = 0;
+  if ((s = check_view({names[0], k, k_sb, k_st, n, 2}, B, hd, &kb)) != FASTVR_OK) return s;
+  if ((s = check_view({names[1], v, v_sb, v_st, n, 2}, B, hd, &vb)) != FASTVR_OK) return s;
+  if (starts != nullptr) sb = B * 4;
+  int i;
+  if ((i = kv4_overlap(t, k, kb)) >= 0)
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "%s overlaps %s", kKv4Names[i], names[0]);
+  if ((i = kv4_overlap(t, v, vb)) >= 0)
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "%s overlaps %s", kKv4Names[i], names[1]);
+  if (write) {
+    if ((i = kv4_overlap(t, starts, sb)) >= 0)
+      return fail(FASTVR_ERR_INVALID_ARGUMENT, "%s overlaps starts", kKv4Names[i]);
+    for (int a = 0; a < 4; ++a)
+      for (int b = a + 1; b < 4; ++b)
+        if (t.bytes[a] > 0 && overlap(t.ptr[a], t.bytes[a], t.ptr[b], t.bytes[b]))
+          return fail(FASTVR_ERR_INVALID_ARGUMENT, "%s overlaps %s", kKv4Names[a], kKv4Names[b]);
+  } else {
+    // K and V side by side in one token row (views of one buffer) interleave without overlap
+    const char *kp = static_cast<const char*>(k), *vp = static_cast<const char*>(v);
+    const uintptr_t gap = kp < vp ? uintptr_t(vp - kp) : uintptr_t(kp - vp);
+    const bool beside = k_st == v_st && (B == 1 || k_sb == v_sb) && gap >= uintptr_t(hd * 2) &&
+                        gap + uintptr_t(hd * 2) <= uintptr_t(k_st * 2);
+    if (!beside && overlap(k, kb, v, vb)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "k_out overlaps v_out");
+    if (sb > 0 && (overlap(starts, sb, k, kb) || overlap(starts, sb, v, vb)))
+      return fail(FASTVR_ERR_INVALID_ARGUMENT, "starts overlaps k_out or v_out");
+  }
+  fastvr::Kv4CopyArgs a;
+  a.cache = {const_cast<void*>(kc), const_cast<void*>(ks), const_cast<void*>(vc), const_cast<void*>(vs)};
+  a.k = const_cast<void*>(k); a.v = const_cast<void*>(v);
+  a.k_sb = k_sb; a.k_st = k_st; a.v_sb = v_sb; a.v_st = v_st;
+  a.starts = starts;
+  a.B = B; a.H = H; a.d = d; a.capacity = capacity;
+  a.first = starts == nullptr ? first : 0;
+  a.n = n;
+  const char* what = write ? "kv4_append" : "kv4_read";
+  if ((write ? fastvr::launch_kv4_append : fastvr::launch_kv4_read) == nullptr) return no_kernels(what);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const hipError_t e = write ? fastvr::launch_kv4_append(a, st) : fastvr::launch_kv4_read(a, st);
+  if (e != hipSuccess) return fail(FASTVR_ERR_HIP, "%s launch failed: %s", what, hipGetErrorString(e));
+  return ok();
+}
+
+// Sizes and mask of an attention over a 4-bit cache; *empty: nothing to do.
+fastvr_status kv4_sizes(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d, int64_t cache_len,
+                        int64_t chunk_len, int64_t window_chunks, bool* empty) {
+  *empty = false;
+  if (B < 0 || H < 0 || Hkv < 0 || Nq < 0 || cache_len < 0)
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "negative size (B=%lld H=%lld Hkv=%lld Nq=%lld cache_len=%lld)",
+                (long long)B, (long long)H, (long long)Hkv, (long long)Nq, (long long)cache_len);
+  if (d != 64 && d != 128) return fail(FASTVR_ERR_UNSUPPORTED, "head_dim %lld not in {64, 128}", (long long)d);
+  if (H > 0 && (Hkv < 1 || H % Hkv != 0))
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "H = %lld is not a multiple of Hkv = %lld", (long long)H, (long long)Hkv);
+  if (chunk_len < 1) return fail(FASTVR_ERR_INVALID_ARGUMENT, "chunk_len %lld < 1", (long long)chunk_len);
+  if (window_chunks < -1)
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "window_chunks %lld < -1", (long long)window_chunks);
+  if (cache_len > FASTVR_KV4_MAX_CAPACITY)
+    return fail(FASTVR_ERR_UNSUPPORTED, "cache_len %lld > %lld", (long long)cache_len,
+                (long long)FASTVR_KV4_MAX_CAPACITY);
+  if (B == 0 || H == 0 || Nq == 0) {
+    *empty = true;
+    return FASTVR_OK;
+  }
+  int64_t rows;
+  if (B > INT32_MAX || H > INT32_MAX || Nq > INT32_MAX || !mul_ok(Nq, H, &rows) || rows > INT32_MAX ||
+      !mul_ok(rows, B, &rows) || rows > (int64_t(1) << 36))
+    return fail(FASTVR_ERR_UNSUPPORTED, "sizes must be below 2^31, and B * H * Nq below 2^36");
+  const fastvr::Kv4Plan plan = fastvr::kv4_plan(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks);
+  if (plan.units > fastvr::kMaxKv4Units || rows > fastvr::kMaxKv4Units * 4)
+    return fail(FASTVR_ERR_UNSUPPORTED, "problem needs too many workgroups");
+  return FASTVR_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+fastvr_status fastvr_rope(const void* x, int64_t x_sb, int64_t x_st, int32_t x_fp32, void* y, int64_t y_sb,
+                          int64_t y_st, int32_t y_fp32, const int32_t* positions, int64_t pos_sb, int64_t n_axes,
+                          int64_t split1, int64_t split2, const double* inv_freq, int64_t n_pairs, double amplitude,
+                          int32_t interleaved, int32_t inverse, int64_t B, int64_t N, int64_t H, int64_t d,
+                          void* stream) {
+  if (B < 0 || N < 0 || H < 0)
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "negative size (B=%lld N=%lld H=%lld)", (long long)B, (long long)N,
+                (long long)H);
+  if (d != 64 && d != 128) return fail(FASTVR_ERR_UNSUPPORTED, "head_dim %lld not in {64, 128}", (long long)d);
+  const int32_t flags[4] = {x_fp32, y_fp32, interleaved, inverse};
+  const char* const flag_names[4] = {"x_fp32", "y_fp32", "interleaved", "inverse"};
+  for (int i = 0; i < 4; ++i)
+    if (flags[i] != 0 && flags[i] != 1)
+      return fail(FASTVR_ERR_INVALID_ARGUMENT, "%s must be 0 or 1 (got %d)", flag_names[i], (int)flags[i]);
+  if (n_pairs < 0 || n_pairs > d / 2)
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "n_pairs %lld not in 0 .. d / 2", (long long)n_pairs);
+  if (n_axes < 1 || n_axes > 3) return fail(FASTVR_ERR_INVALID_ARGUMENT, "n_axes %lld not in 1 .. 3", (long long)n_axes);
+  if (split1 < 0 || split2 < split1 || n_pairs < split2 || (n_axes == 1 && split1 != n_pairs) ||
+      (n_axes == 2 && split2 != n_pairs))
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "axes: split1 = %lld, split2 = %lld of %lld pairs, %lld axes",
+                (long long)split1, (long long)split2, (long long)n_pairs, (long long)n_axes);
+  if (!std::isfinite(amplitude) || !std::isfinite(static_cast<float>(amplitude)))
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "amplitude is not finite");
+  if (B == 0 || N == 0 || H == 0) return ok();
+  int64_t hd, size;
+  if (!mul_ok(H, d, &hd) || !mul_ok(N, hd, &size)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "size overflows int64");
+  if (B > 65535 || size >= (int64_t(1) << 33))
+    return fail(FASTVR_ERR_UNSUPPORTED, "B > 65535 or N * H * d >= 2^33");
+  int64_t xb, yb, pb, fb;
+  fastvr_status s;
+  if ((s = check_view({"x", x, x_sb, x_st, N, x_fp32 ? 4 : 2}, B, hd, &xb)) != FASTVR_OK) return s;
+  if ((s = check_view({"y", y, y_sb, y_st, N, y_fp32 ? 4 : 2}, B, hd, &yb)) != FASTVR_OK) return s;
+  if (positions == nullptr) return fail(FASTVR_ERR_INVALID_ARGUMENT, "positions is NULL");
+  if (!aligned(positions, 4)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "positions is not 4-byte aligned");
+  if (pos_sb != 0 && pos_sb < N * n_axes)
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "positions batch stride %lld < N * n_axes = %lld", (long long)pos_sb,
+                (long long)(N * n_axes));
+  if (!mul_ok(B - 1, pos_sb, &pb) || !add_ok(pb, N * n_axes, &pb) || !mul_ok(pb, 4, &pb))
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "positions size overflows int64");
+  if (n_pairs > 0 && inv_freq == nullptr) return fail(FASTVR_ERR_INVALID_ARGUMENT, "inv_freq is NULL");
+  if (!aligned(inv_freq, 8)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "inv_freq is not 8-byte aligned");
+  fb = n_pairs * 8;
+  const bool in_place = y == x && y_fp32 == x_fp32 && y_st == x_st && (B == 1 || y_sb == x_sb);
+  if (!in_place && overlap(y, yb, x, xb)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "y overlaps x");
+  if (overlap(y, yb, positions, pb)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "y overlaps positions");
+  if (fb > 0 && overlap(y, yb, inv_freq, fb)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "y overlaps inv_freq");
+  fastvr::RopeArgs a;
+  a.x = x; a.y = y;
+  a.x_sb = x_sb; a.x_st = x_st; a.y_sb = y_sb; a.y_st = y_st;
+  a.x_fp32 = x_fp32 == 1; a.y_fp32 = y_fp32 == 1;
+  a.positions = positions;
+  a.pos_sb = pos_sb; a.n_axes = n_axes; a.split1 = split1; a.split2 = split2;
+  a.inv_freq = inv_freq;
+  a.n_pairs = n_pairs;
+  a.amplitude = static_cast<float>(amplitude);
+  a.interleaved = interleaved == 1; a.inverse = inverse == 1;
+  a.B = B; a.N = N; a.H = H; a.d = d;
+  if (fastvr::launch_rope == nullptr) return no_kernels("rope");
+  const hipError_t e = fastvr::launch_rope(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(FASTVR_ERR_HIP, "rope launch failed: %s", hipGetErrorString(e));
+  return ok();
+}
+
+fastvr_status fastvr_kv4_append(void* k_codes, void* k_scales, void* v_codes, void* v_scales, const void* k_new,
+                                int64_t k_sb, int64_t k_st, const void* v_new, int64_t v_sb, int64_t v_st,
+                                const int32_t* starts, int64_t B, int64_t H, int64_t d, int64_t capacity,
+                                int64_t first, int64_t n_new, void* stream) {
+  return kv4_copy(true, k_codes, k_scales, v_codes, v_scales, k_new, k_sb, k_st, v_new, v_sb, v_st, starts, B, H, d,
+                  capacity, first, n_new, stream);
+}
+
+fastvr_status fastvr_kv4_read(const void* k_codes, const void* k_scales, const void* v_codes, const void* v_scales,
+                              void* k_out, int64_t k_sb, int64_t k_st, void* v_out, int64_t v_sb, int64_t v_st,
+                              const int32_t* starts, int64_t B, int64_t H, int64_t d, int64_t capacity, int64_t first,
+                              int64_t n, void* stream) {
+  return kv4_copy(false, k_codes, k_scales, v_codes, v_scales, k_out, k_sb, k_st, v_out, v_sb, v_st, starts, B, H, d,
+                  capacity, first, n, stream);
+}
+
+fastvr_status fastvr_kv4_attn_workspace(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d, int64_t cache_len,
+                                        int64_t chunk_len, int64_t window_chunks, int64_t* bytes) {
+  if (bytes == nullptr) return fail(FASTVR_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  bool empty;
+  const fastvr_status s = kv4_sizes(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks, &empty);
+  if (s != FASTVR_OK) return s;
+  *bytes = empty ? 0 : fastvr::kv4_plan(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks).ws_bytes;
+  return ok();
+}
+
+fastvr_status fastvr_kv4_attn(const void* q, int64_t q_sb, int64_t q_st, const void* k_codes, const void* k_scales,
+                              const void* v_codes, const void* v_scales, void* o, int64_t o_sb, int64_t o_st,
+                              int32_t o_bf16, float* lse, void* workspace, int64_t workspace_bytes,
+                              const int32_t* lens, int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d,
+                              int64_t capacity, int64_t cache_len, int64_t chunk_len, int64_t window_chunks,
+                              float scale, void* stream) {
+  bool empty;
+  fastvr_status s = kv4_sizes(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks, &empty);
+  if (s != FASTVR_OK) return s;
+  if (capacity < cache_len)
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "cache_len = %lld > capacity = %lld", (long long)cache_len,
+                (long long)capacity);
+  if (capacity > FASTVR_KV4_MAX_CAPACITY)
+    return fail(FASTVR_ERR_UNSUPPORTED, "capacity %lld > %lld", (long long)capacity,
+                (long long)FASTVR_KV4_MAX_CAPACITY);
+  if (!std::isfinite(scale)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "scale is not finite");
+  if (o_bf16 != 0 && o_bf16 != 1)
+    return fail(FASTVR_ERR_INVALID_ARGUMENT, "o_bf16 must be 0 or 1 (got %d)", (int)o_bf16);
+  if (empty) return ok();
+  Kv4Tensors t;
+  if ((s = check_kv4(k_codes, k_scales, v_codes, v_scales, B, Hkv, d, capacity, &t)) != FASTVR_OK) return s;
+  const int64_t hd = H * d;
+  int64_t qb, ob, lb = 0;
+  if ((s = check_view({"q", q, q_sb, q_st, Nq, 2}, B, hd, &qb)) != FASTVR_OK) return s;
+  if ((s = check_view({"o", o, o_sb, o_st, Nq, o_bf16 ? 2 : 4}, B, hd, &ob)) != FASTVR_OK) return s;
+  if (q_st > INT32_MAX || o_st > INT32_MAX)
+    return fail(FASTVR_ERR_UNSUPPORTED, "token strides must be below 2^31 elements");
+  if (lse != nullptr) {
+    if (!aligned(lse, 4)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "lse is not 4-byte aligned");
+    lb = B * H * Nq * 4;
+  }
+  if (!aligned(lens, 4)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "lens is not 4-byte aligned");
+  const fastvr::Kv4Plan plan = fastvr::kv4_plan(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks);
+  if (plan.ws_bytes > 0) {
+    if (workspace == nullptr || workspace_bytes < plan.ws_bytes)
+      return fail(FASTVR_ERR_INVALID_ARGUMENT, "workspace of %lld bytes, %lld needed",
+                  (long long)(workspace == nullptr ? 0 : workspace_bytes), (long long)plan.ws_bytes);
+    if (!aligned(workspace, 16)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "workspace is not 16-byte aligned");
+  }
+  // what the call writes overlaps nothing else
+  const void* ptrs[5] = {o, lse, workspace, q, lens};
+  const int64_t sizes[5] = {ob, lb, plan.ws_bytes, qb, lens != nullptr ? B * 4 : 0};
+  const char* const names[5] = {"o", "lse", "workspace", "q", "lens"};
+  for (int w = 0; w < 3; ++w) {
+    if (sizes[w] == 0) continue;
+    for (int i = w + 1; i < 5; ++i)
+      if (sizes[i] > 0 && overlap(ptrs[w], sizes[w], ptrs[i], sizes[i]))
+        return fail(FASTVR_ERR_INVALID_ARGUMENT, "%s overlaps %s", names[w], names[i]);
+    const int c = kv4_overlap(t, ptrs[w], sizes[w]);
+    if (c >= 0) return fail(FASTVR_ERR_INVALID_ARGUMENT, "%s overlaps %s", names[w], kKv4Names[c]);
+  }
+  fastvr::Kv4AttnArgs a;
+  a.q = q;
+  a.q_sb = q_sb; a.q_st = q_st;
+  a.cache = {const_cast<void*>(k_codes), const_cast<void*>(k_scales), const_cast<void*>(v_codes),
+             const_cast<void*>(v_scales)};
+  a.o = o;
+  a.o_sb = o_sb; a.o_st = o_st;
+  a.o_bf16 = o_bf16 == 1;
+  a.lse = lse;
+  a.workspace = workspace;
+  a.lens = lens;
+  a.B = B; a.H = H; a.Hkv = Hkv; a.nq = Nq; a.d = d;
+  a.capacity = capacity; a.cache_len = cache_len;
+  a.chunk_len = chunk_len; a.window_chunks = window_chunks;
+  a.scale = scale;
+  if (fastvr::launch_kv4_attn == nullptr) return no_kernels("kv4_attn");
+  const hipError_t e = fastvr::launch_kv4_attn(a, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return fail(FASTVR_ERR_HIP, "kv4_attn launch failed: %s", hipGetErrorString(e));
+  return ok();
 }
 
 const char* fastvr_status_string(fastvr_status s) {

@@ -1,0 +1,500 @@
+// Attention over a KV cache in 4 bits: from one token of each sequence to whole
+// chunks, with grouped heads and a length per sequence.
+//
+//   O_i = sum_j exp(scale q_i . k_j - LSE_i) v_j,  LSE_i = ln sum_j exp(scale q_i . k_j)
+//
+// over the keys that row i sees, a contiguous interval [lo_i, hi_i).  The rows of one
+// key head are (token, head of the group) pairs in that order, so lo and hi do not
+// fall from row to row.  A workgroup takes a tile of 16 or 32 rows of one (batch,
+// key head) and a share of the keys that the tile sees; its four waves take steps of
+// 32 keys in turn, each with its own running maximum, sum and O, and join them
+// through LDS.  Where the tiles are few, the keys are split over several workgroups
+// and a second kernel joins their partial results (kv4_plan.h).
+//
+// A step, one wave: S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_16x16x32_bf16.
+//  * K comes from the cache straight into registers: a lane holds a quarter of a key
+//    row, which four (two) converting instructions per dword turn into the A operand
+//    in place (the order of head_dim along the reduction is free, Q is loaded in the
+//    same one).
+//  * S^T puts one row of the tile on a lane and 8 of the 32 keys on each of the four
+//    lanes of that row; rounded to bf16 these 8 are the B operand of O^T as they are,
+//    when V's operand holds the same 8 keys: two runs of 4.
+//  * V: a lane converts the same 8 (4) elements of those 8 keys and swaps halves
+//    between neighbouring keys (v_perm) to get, per element, 8 keys in a row.
+//  * The maximum a row is measured against is raised only when a score exceeds it by
+//    8 (in log2 units: P <= 2^8 then), so that most steps need no exchange between
+//    lanes and no rescale of O.
+// A step is about 200 vector instructions against 256 cycles of matrix core: for one
+// row tile, reading the cache from HBM takes longer than both.
+//
+// Keys a row does not see: their P is zero, and in the steps where that can happen
+// V blocks that are not finite (rows behind a sequence may hold anything) are taken
+// as zero, and NaN is put into the O of the rows that do see them.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "class_plan.h"
+#include "gfx950_ops.h"
+#include "kv4.h"
+#include "kv4_plan.h"
+#include "launch.h"
+
+namespace fastvr {
+namespace {
+
+using namespace dev;
+
+constexpr int kThreads = 64 * kKv4Waves;
+constexpr float kInf = __builtin_inff();
+constexpr float kSlack = 8.f;  // log2 units a score may exceed the running reference by
+
+struct Kv4Params {
+  const uint16_t* q;
+  int64_t q_sb;
+  int32_t q_st;
+  const uint8_t *k_codes, *k_scales, *v_codes, *v_scales;
+  void* o;
+  int64_t o_sb;
+  int32_t o_st;
+  int32_t o_bf16;
+  float* lse;
+  float* part;  // [row][split][D] unnormalised O, then [row][split] (maximum, sum)
+  const int32_t* lens;
+  int32_t B, H, Hkv, G, nq, R, capacity, cache_len, chunk_len, window;
+  int32_t row_tiles, n_split, units;
+  int64_t rows;
+  float c;  // |scale| * log2(e)
+  uint32_t sign;  // flips q for a negative scale
+};
+
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                 0);
+}
+
+// x of the lanes l and l ^ 16, in both of them
+__device__ __forceinline__ float swap_rows(float x, float* other) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x),
+                                                  false, false);
+  *other = __builtin_bit_cast(float, (uint32_t)r[1]);
+  return __builtin_bit_cast(float, (uint32_t)r[0]);
+}
+// maximum and sum over the four lanes of a row
+__device__ __forceinline__ float row_max4(float x) {
+  float o;
+  x = swap_rows(x, &o);
+  x = __builtin_fmaxf(x, o);
+  x = swap_halves(x, &o);
+  return __builtin_fmaxf(x, o);
+}
+__device__ __forceinline__ float row_sum4(float x) {
+  float o;
+  x = swap_rows(x, &o);
+  x += o;
+  x = swap_halves(x, &o);
+  return x + o;
+}
+
+// Keys [lo, hi) that the token at `pos` sees, of len.
+__device__ __forceinline__ void interval(const Kv4Params& p, int pos, int len, int& lo, int& hi) {
+  lo = hi = 0;
+  if (pos < 0) return;
+  const int c = pos / p.chunk_len, first = c * p.chunk_len;
+  lo = (p.window >= 0 && c > p.window) ? first - p.window * p.chunk_len : 0;
+  hi = len - first > p.chunk_len ? first + p.chunk_len : len;
+}
+
+template <int D>
+struct Step {  // what a lane loads for 32 keys
+  static constexpr int kK = D / 32;   // dwords of K a lane holds per key
+  uint32_t k[2][kK];
+  uint32_t ks[2];
+  uint32_t v[8];
+  uint32_t vs[8];
+};
+
+template <int D, int QT>
+__global__ __launch_bounds__(kThreads) void kv4_attn_kernel(const Kv4Params p) {
+  constexpr int kE = D / 16;    // elements of V a lane holds per key; O^T tiles
+  constexpr int kKK = D / 32;   // reduction steps of S
+  constexpr int kPitch = D + 4;
+  constexpr int kRows = 16 * QT;
+  __shared__ __attribute__((aligned(16))) float sm_o[kKv4Waves * 16 * kPitch];
+  __shared__ float sm_m[kKv4Waves * kRows], sm_l[kKv4Waves * kRows];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  // workgroup -> (batch, key head), split, row tile; row tiles of one key range run
+  // next to each other on one XCD and share its L2
+  const int u = p.row_tiles > 1 ? xcd_unit(blockIdx.x, p.units) : (int)blockIdx.x;
+  const int tile = u % p.row_tiles, us = u / p.row_tiles;
+  const int split = us % p.n_split, bh = us / p.n_split;
+  const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
+  int len = p.cache_len;
+  if (p.lens != nullptr) {
+    const int l = p.lens[b];
+    len = l < 0 ? 0 : (l < len ? l : len);
+  }
+
+  // rows of this lane
+  const int row0 = tile * kRows;
+  const int row_last = (row0 + kRows < p.R ? row0 + kRows : p.R) - 1;
+  int lo_min, hi_min, lo_max, hi_max;
+  interval(p, len - p.nq + row0 / p.G, len, lo_min, hi_min);
+  interval(p, len - p.nq + row_last / p.G, len, lo_max, hi_max);
+
+  u32x4 q[QT][kKK];
+  int lo[QT], hi[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    const int r = row0 + t * 16 + n;
+    const bool have = r <= row_last;
+    const int i = (have ? r : row_last) / p.G;
+    const int h = hk * p.G + (have ? r : row_last) - i * p.G;
+    interval(p, len - p.nq + i, len, lo[t], hi[t]);
+    const uint16_t* src = p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_st + h * D + g * (D / 4);
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk) {
+      q[t][kk] = *reinterpret_cast<const u32x4*>(src + kk * 8);
+      q[t][kk] ^= p.sign;
+    }
+  }
+
+  f32x4 acc[QT][kE];
+  float mc[QT], l[QT];  // reference in log2 units, sum of this lane's keys
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    mc[t] = -kInf;
+    l[t] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kE; ++j) acc[t][j] = f32x4{};
+  }
+
+  const int64_t slab = (int64_t)bh * p.capacity;
+  const __amdgpu_buffer_rsrc_t rkc = make_rsrc(p.k_codes + slab * (D / 2), (int64_t)p.capacity * (D / 2));
+  const __amdgpu_buffer_rsrc_t rks = make_rsrc(p.k_scales + slab * (D / 32), (int64_t)p.capacity * (D / 32));
+  const __amdgpu_buffer_rsrc_t rvc = make_rsrc(p.v_codes + slab * (D / 2), (int64_t)p.capacity * (D / 2));
+  const __amdgpu_buffer_rsrc_t rvs = make_rsrc(p.v_scales + slab * (D / 32), (int64_t)p.capacity * (D / 32));
+  const uint32_t kc_off = n * (D / 2) + g * (D / 8), ks_off = n * (D / 32) + (D == 128 ? g : g >> 1);
+  const uint32_t vc_off = 4 * g * (D / 2) + n * (D / 32), vs_off = 4 * g * (D / 32) + n * kE / 32;
+
+  // rows behind the cache's capacity read as zero
+  auto load = [&](int st, Step<D>& s) {
+    const uint32_t k0 = (uint32_t)st * kKv4StepKeys;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const uint32_t off = (k0 + 16 * x) * (D / 2) + kc_off;
+      if (D == 128) {
+        const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rkc, off, 0, 0));
+#pragma unroll
+        for (int i = 0; i < kKK; ++i) s.k[x][i] = w[i];
+      } else {
+        const auto w = __builtin_amdgcn_raw_buffer_load_b64(rkc, off, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kKK; ++i) s.k[x][i] = w[i];
+      }
+      s.ks[x] = __builtin_amdgcn_raw_buffer_load_b8(rks, (k0 + 16 * x) * (D / 32) + ks_off, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t key = k0 + (i & 3) + 16 * (i >> 2);
+      if (D == 128)
+        s.v[i] = __builtin_amdgcn_raw_buffer_load_b32(rvc, key * (D / 2) + vc_off, 0, 0);
+      else
+        s.v[i] = __builtin_amdgcn_raw_buffer_load_b16(rvc, key * (D / 2) + vc_off, 0, 0);
+      s.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(rvs, key * (D / 32) + vs_off, 0, 0);
+    }
+  };
+
+  auto compute = [&](int st, const Step<D>& s, auto masked) {
+    constexpr bool MASK = decltype(masked)::value;
+    const int k0 = st * kKv4StepKeys;
+    f32x4 sc[QT][2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float scale = kv4_scale(s.ks[x]);
+#pragma unroll
+      for (int kk = 0; kk < kKK; ++kk) {
+        const u32x4 a = kv4_values(s.k[x][kk], scale);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) sc[t][x] = mfma16(a, q[t][kk], kk == 0 ? f32x4{} : sc[t][x]);
+      }
+    }
+    u32x4 pf[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float m = -kInf;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (MASK) {
+            const int key = k0 + 16 * x + 4 * g + r;
+            if (key < lo[t] || key >= hi[t]) sc[t][x][r] = -kInf;
+          }
+          m = __builtin_fmaxf(m, sc[t][x][r]);
+        }
+      if (__builtin_amdgcn_ballot_w64(m * p.c > mc[t] + kSlack)) {
+        // raise the reference of every row to its maximum so far (fmaxf drops the NaN of
+        // -inf * 0, and of scores)
+        const float m_new = __builtin_fmaxf(mc[t], row_max4(m) * p.c);
+        const float alpha = mc[t] == -kInf ? 0.f : __builtin_amdgcn_exp2f(mc[t] - m_new);
+        mc[t] = m_new;
+        l[t] *= alpha;
+#pragma unroll
+        for (int j = 0; j < kE; ++j) acc[t][j] *= alpha;
+      }
+      const float nm = mc[t] == -kInf ? 0.f : -mc[t];
+      bf16x8 pb;
+      float sum = 0.f;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][x][r], p.c, nm));
+          if (MASK) {
+            const int key = k0 + 16 * x + 4 * g + r;
+            e = (key < lo[t] || key >= hi[t]) ? 0.f : e;
+          }
+          sum += e;
+          pb[4 * x + r] = (__bf16)e;
+        }
+      l[t] += sum;
+      pf[t] = __builtin_bit_cast(u32x4, pb);
+    }
+    // V: keys 4 g + (0..3) and 16 + 4 g + (0..3), elements n * kE ..
+    uint32_t w[8][kE / 2];
+    bool nan_block = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t byte = s.vs[i], code = s.v[i];
+      if (MASK && byte > 252u) {
+        nan_block = true;
+        byte = 127u;
+        code = 0u;
+      }
+      const float scale = kv4_scale(byte);
+      w[i][0] = kv4_pair<0>(code, scale);
+      w[i][1] = kv4_pair<1>(code, scale);
+      if (D == 128) {
+        w[i][kE / 2 - 2] = kv4_pair<2>(code, scale);
+        w[i][kE / 2 - 1] = kv4_pair<3>(code, scale);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kE; ++j) {
+      u32x4 a;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        a[i] = __builtin_amdgcn_perm(w[2 * i + 1][j / 2], w[2 * i][j / 2], (j & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) acc[t][j] = mfma16(a, pf[t], acc[t][j]);
+    }
+    if (MASK && __builtin_amdgcn_ballot_w64(nan_block)) {
+      // this lane's O holds one 32-element block of one row: block g (head_dim 128), g / 2 (64)
+      for (int i = 0; i < kKv4StepKeys; ++i) {
+        const int key = k0 + i;
+        const uint32_t byte = __builtin_amdgcn_raw_buffer_load_b8(
+            rvs, (uint32_t)key * (D / 32) + (D == 128 ? g : g >> 1), 0, 0);
+#pragma unroll
+        for (int t = 0; t < QT; ++t)
+          if (byte > 252u && key >= lo[t] && key < hi[t])
+#pragma unroll
+            for (int j = 0; j < kE; ++j) acc[t][j] += __builtin_nanf("");
+      }
+    }
+  };
+
+  if (hi_max > lo_min) {
+    const int s0 = lo_min / kKv4StepKeys;
+    const int n_steps = (hi_max + kKv4StepKeys - 1) / kKv4StepKeys - s0;
+    const int begin = s0 + (int)((int64_t)n_steps * split / p.n_split);
+    const int end = s0 + (int)((int64_t)n_steps * (split + 1) / p.n_split);
+    Step<D> cur, next;
+    int st = begin + wave;
+    if (st < end) load(st, cur);
+    for (; st < end; st += kKv4Waves) {
+      if (st + kKv4Waves < end) load(st + kKv4Waves, next);
+      const int k0 = st * kKv4StepKeys;
+      // all rows see all keys of the step
+      if (k0 >= lo_max && k0 + kKv4StepKeys <= hi_min)
+        compute(st, cur, std::false_type{});
+      else
+        compute(st, cur, std::true_type{});
+      cur = next;
+    }
+  }
+
+  // join the waves
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    l[t] = row_sum4(l[t]);
+    if (g == 0) {
+      sm_m[wave * kRows + t * 16 + n] = mc[t];
+      sm_l[wave * kRows + t * 16 + n] = l[t];
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    __syncthreads();
+    {
+      float m = -kInf;
+#pragma unroll
+      for (int w = 0; w < kKv4Waves; ++w) m = __builtin_fmaxf(m, sm_m[w * kRows + t * 16 + n]);
+      const float f = mc[t] == -kInf ? (l[t] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(mc[t] - m);
+      float* dst = sm_o + (wave * 16 + n) * kPitch;
+      // element n' * kE + j of O^T row n' = 4 g + r
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int j = 0; j < kE; j += 4)
+          *reinterpret_cast<f32x4*>(dst + (4 * g + r) * kE + j) =
+              f32x4{acc[t][j][r] * f, acc[t][j + 1][r] * f, acc[t][j + 2][r] * f, acc[t][j + 3][r] * f};
+    }
+    __syncthreads();
+    const int rr = tid >> 4, e0 = (tid & 15) * kE;
+    const int r = row0 + t * 16 + rr;
+    if (r < p.R) {
+      float m = -kInf, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kKv4Waves; ++w) m = __builtin_fmaxf(m, sm_m[w * kRows + t * 16 + rr]);
+#pragma unroll
+      for (int w = 0; w < kKv4Waves; ++w) {
+        const float mw = sm_m[w * kRows + t * 16 + rr], lw = sm_l[w * kRows + t * 16 + rr];
+        sum += mw == -kInf ? lw : lw * __builtin_amdgcn_exp2f(mw - m);
+      }
+      float v[kE];
+#pragma unroll
+      for (int j = 0; j < kE; ++j) {
+        v[j] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kKv4Waves; ++w) v[j] += sm_o[(w * 16 + rr) * kPitch + e0 + j];
+      }
+      const int i = r / p.G, h = hk * p.G + r - i * p.G;
+      const int64_t out_row = ((int64_t)b * p.H + h) * p.nq + i;
+      if (p.n_split > 1) {
+        float* dst = p.part + (out_row * p.n_split + split) * D + e0;
+#pragma unroll
+        for (int j = 0; j < kE; j += 4) *reinterpret_cast<f32x4*>(dst + j) = f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]};
+        if (e0 == 0) {
+          float* ml = p.part + p.rows * p.n_split * D + (out_row * p.n_split + split) * 2;
+          ml[0] = m;
+          ml[1] = sum;
+        }
+      } else {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int64_t e = (int64_t)b * p.o_sb + (int64_t)i * p.o_st + h * D + e0;
+        if (p.o_bf16) {
+          __bf16* dst = static_cast<__bf16*>(p.o) + e;
+#pragma unroll
+          for (int j = 0; j < kE; ++j) dst[j] = (__bf16)(v[j] * inv);
+        } else {
+          float* dst = static_cast<float*>(p.o) + e;
+#pragma unroll
+          for (int j = 0; j < kE; ++j) dst[j] = v[j] * inv;
+        }
+        if (e0 == 0 && p.lse != nullptr) p.lse[out_row] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
+      }
+    }
+  }
+}
+
+// Joins the partial results of a row's splits: one wave a row, D / 64 elements a lane.
+template <int D>
+__global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
+  constexpr int kE = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * kKv4Waves + (threadIdx.x >> 6);
+  if (row >= p.rows) return;
+  const float* ml = p.part + p.rows * p.n_split * D + row * p.n_split * 2;
+  // lane s holds split s (n_split <= 64)
+  const float m_s = lane < p.n_split ? ml[2 * lane] : -kInf;
+  const float l_s = lane < p.n_split ? ml[2 * lane + 1] : 0.f;
+  float m = m_s;
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, x));
+  const float f = m_s == -kInf ? (l_s == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m_s - m);
+  float sum = l_s * f;
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+  float v[kE] = {};
+  const float* src = p.part + row * p.n_split * D + lane * kE;
+  for (int s = 0; s < p.n_split; ++s) {
+    const float w = __shfl(f, s);
+#pragma unroll
+    for (int j = 0; j < kE; ++j) v[j] += w * src[s * D + j];
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int i = (int)(row % p.nq);
+  const int64_t bh = row / p.nq;
+  const int h = (int)(bh % p.H);
+  const int64_t e = bh / p.H * p.o_sb + (int64_t)i * p.o_st + h * D + lane * kE;
+#pragma unroll
+  for (int j = 0; j < kE; ++j) {
+    if (p.o_bf16)
+      static_cast<__bf16*>(p.o)[e + j] = (__bf16)(v[j] * inv);
+    else
+      static_cast<float*>(p.o)[e + j] = v[j] * inv;
+  }
+  if (lane == 0 && p.lse != nullptr) p.lse[row] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
+}
+
+template <int D>
+hipError_t launch_t(const Kv4Params& p, const Kv4Plan& plan, hipStream_t stream) {
+  const dim3 grid((unsigned)plan.units), block(kThreads);
+  if (plan.q_tiles == 1)
+    hipLaunchKernelGGL((kv4_attn_kernel<D, 1>), grid, block, 0, stream, p);
+  else
+    hipLaunchKernelGGL((kv4_attn_kernel<D, 2>), grid, block, 0, stream, p);
+  if (plan.n_split > 1) {
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const dim3 rows((unsigned)((plan.rows + kKv4Waves - 1) / kKv4Waves));
+    hipLaunchKernelGGL(kv4_join_kernel<D>, rows, block, 0, stream, p);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t stream) {
+  const Kv4Plan plan = kv4_plan(a.B, a.H, a.Hkv, a.nq, a.d, a.cache_len, a.chunk_len, a.window_chunks);
+  Kv4Params p;
+  p.q = static_cast<const uint16_t*>(a.q);
+  p.q_sb = a.q_sb;
+  p.q_st = (int32_t)a.q_st;
+  p.k_codes = static_cast<const uint8_t*>(a.cache.k_codes);
+  p.k_scales = static_cast<const uint8_t*>(a.cache.k_scales);
+  p.v_codes = static_cast<const uint8_t*>(a.cache.v_codes);
+  p.v_scales = static_cast<const uint8_t*>(a.cache.v_scales);
+  p.o = a.o;
+  p.o_sb = a.o_sb;
+  p.o_st = (int32_t)a.o_st;
+  p.o_bf16 = a.o_bf16 ? 1 : 0;
+  p.lse = a.lse;
+  p.part = static_cast<float*>(a.workspace);
+  p.lens = a.lens;
+  p.B = (int32_t)a.B;
+  p.H = (int32_t)a.H;
+  p.Hkv = (int32_t)a.Hkv;
+  p.G = (int32_t)(a.H / a.Hkv);
+  p.nq = (int32_t)a.nq;
+  p.R = (int32_t)(a.nq * p.G);
+  p.capacity = (int32_t)a.capacity;
+  p.cache_len = (int32_t)a.cache_len;
+  // a chunk longer than the cache is a chunk of the whole cache, a window past the
+  // first chunk unbounded
+  const int64_t L = a.chunk_len > a.cache_len ? (a.cache_len > 0 ? a.cache_len : 1) : a.chunk_len;
+  p.chunk_len = (int32_t)L;
+  p.window = (int32_t)(a.window_chunks > a.cache_len / L ? -1 : a.window_chunks);
+  p.row_tiles = (int32_t)plan.row_tiles;
+  p.n_split = plan.n_split;
+  p.units = (int32_t)plan.units;
+  p.rows = plan.rows;
+  p.c = __builtin_fabsf(a.scale) * 1.44269504088896340736f;
+  p.sign = a.scale < 0.f ? 0x80008000u : 0u;
+  return a.d == 128 ? launch_t<128>(p, plan, stream) : launch_t<64>(p, plan, stream);
+}
+
+}  // namespace fastvr

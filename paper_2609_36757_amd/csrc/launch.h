@@ -112,4 +112,52 @@ hipError_t launch_kv_append(void* k_cache, void* v_cache, const void* k_new, con
                             int64_t B, int64_t H, int64_t d, int64_t capacity, int64_t cache_len,
                             int64_t n_new, hipStream_t stream);
 
+// Rotary positions and the 4-bit cache.  The launchers are weak references: a build
+// of the C-ABI layer without the kernels links, and its calls end in FASTVR_ERR_HIP.
+struct RopeArgs {
+  const void* x;
+  void* y;
+  int64_t x_sb, x_st, y_sb, y_st;  // element strides
+  bool x_fp32, y_fp32;
+  const int32_t* positions;
+  int64_t pos_sb, n_axes, split1, split2;
+  const double* inv_freq;
+  int64_t n_pairs;
+  float amplitude;
+  bool interleaved, inverse;
+  int64_t B, N, H, d;
+};
+__attribute__((weak)) hipError_t launch_rope(const RopeArgs& a, hipStream_t stream);
+
+struct Kv4Cache {
+  void *k_codes, *k_scales, *v_codes, *v_scales;
+};
+// bf16 rows [B, n, H, d] to (append) or from (read) token rows of the cache
+struct Kv4CopyArgs {
+  Kv4Cache cache;
+  void *k, *v;
+  int64_t k_sb, k_st, v_sb, v_st;
+  const int32_t* starts;  // or null: first
+  int64_t B, H, d, capacity, first, n;
+};
+__attribute__((weak)) hipError_t launch_kv4_append(const Kv4CopyArgs& a, hipStream_t stream);
+__attribute__((weak)) hipError_t launch_kv4_read(const Kv4CopyArgs& a, hipStream_t stream);
+
+constexpr int64_t kMaxKv4Units = (int64_t(1) << 32) / 256 - 1;  // 256-thread workgroups of one launch
+
+struct Kv4AttnArgs {
+  const void* q;
+  int64_t q_sb, q_st;
+  Kv4Cache cache;  // read only
+  void* o;
+  int64_t o_sb, o_st;
+  bool o_bf16;
+  float* lse;
+  void* workspace;
+  const int32_t* lens;  // or null
+  int64_t B, H, Hkv, nq, d, capacity, cache_len, chunk_len, window_chunks;
+  float scale;
+};
+__attribute__((weak)) hipError_t launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t stream);
+
 }  // namespace fastvr

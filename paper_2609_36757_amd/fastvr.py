@@ -9,6 +9,7 @@ import ctypes
 import functools
 import math
 import os
+from typing import NamedTuple
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libfastvr.so")
@@ -23,6 +24,7 @@ EXPORTED = ("fastvr_chunk_attn_fwd", "fastvr_chunk_attn_fwd_ex", "fastvr_kv_cach
             "fastvr_chunk_attn_ring_step", "fastvr_chunk_attn_bwd", "fastvr_chunk_attn_bwd_noalloc",
             "fastvr_one_step_update",
             "fastvr_tile_axis", "fastvr_tile_gather", "fastvr_tile_blend", "fastvr_tile_blend_update",
+            "fastvr_rope", "fastvr_kv4_append", "fastvr_kv4_read", "fastvr_kv4_attn_workspace", "fastvr_kv4_attn",
             "fastvr_status_string", "fastvr_last_error", "fastvr_abi_version")
 
 _i64 = ctypes.c_int64
@@ -73,6 +75,19 @@ def load() -> ctypes.CDLL:
     lib.fastvr_tile_blend_update.restype = ctypes.c_int
     lib.fastvr_tile_blend_update.argtypes = [_vp, _vp, _vp, ctypes.c_float, _i64, _i64, _i64, _i64, _i64, _i64,
                                              _i64, _vp]
+    _i32, _f64 = ctypes.c_int32, ctypes.c_double
+    lib.fastvr_rope.restype = ctypes.c_int
+    lib.fastvr_rope.argtypes = [_vp, _i64, _i64, _i32, _vp, _i64, _i64, _i32, _vp, _i64, _i64, _i64, _i64, _vp, _i64,
+                                _f64, _i32, _i32, _i64, _i64, _i64, _i64, _vp]
+    for copy in (lib.fastvr_kv4_append, lib.fastvr_kv4_read):
+        copy.restype = ctypes.c_int
+        copy.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _i64, _i64, _i64, _i64, _i64, _i64,
+                         _vp]
+    lib.fastvr_kv4_attn_workspace.restype = ctypes.c_int
+    lib.fastvr_kv4_attn_workspace.argtypes = [_i64, _i64, _i64, _i64, _i64, _i64, _i64, _i64, ctypes.POINTER(_i64)]
+    lib.fastvr_kv4_attn.restype = ctypes.c_int
+    lib.fastvr_kv4_attn.argtypes = [_vp, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i32, _vp, _vp, _i64, _vp,
+                                    _i64, _i64, _i64, _i64, _i64, _i64, _i64, _i64, _i64, ctypes.c_float, _vp]
     lib.fastvr_status_string.restype = ctypes.c_char_p
     lib.fastvr_status_string.argtypes = [ctypes.c_int]
     lib.fastvr_last_error.restype = ctypes.c_char_p
@@ -156,6 +171,40 @@ def tile_blend_raw(tiles, out, B, T, Hg, Wg, C, tile, overlap, stream=0) -> int:
 
 def tile_blend_update_raw(v_tiles, z_lq, z_hat, sigma, B, T, Hg, Wg, C, tile, overlap, stream=0) -> int:
     return load().fastvr_tile_blend_update(v_tiles, z_lq, z_hat, sigma, B, T, Hg, Wg, C, tile, overlap, stream)
+
+
+def rope_raw(x, x_sb, x_st, x_fp32, y, y_sb, y_st, y_fp32, positions, pos_sb, n_axes, split1, split2, inv_freq, n_pairs,
+             amplitude, interleaved, inverse, B, N, H, d, stream=0) -> int:
+    return load().fastvr_rope(x, x_sb, x_st, x_fp32, y, y_sb, y_st, y_fp32, positions, pos_sb, n_axes, split1, split2,
+                              inv_freq, n_pairs, amplitude, interleaved, inverse, B, N, H, d, stream)
+
+
+def kv4_append_raw(k_codes, k_scales, v_codes, v_scales, k_new, k_sb, k_st, v_new, v_sb, v_st, starts, B, H, d, capacity,
+                   first, n_new, stream=0) -> int:
+    return load().fastvr_kv4_append(k_codes, k_scales, v_codes, v_scales, k_new, k_sb, k_st, v_new, v_sb, v_st, starts,
+                                    B, H, d, capacity, first, n_new, stream)
+
+
+def kv4_read_raw(k_codes, k_scales, v_codes, v_scales, k_out, k_sb, k_st, v_out, v_sb, v_st, starts, B, H, d, capacity,
+                 first, n, stream=0) -> int:
+    return load().fastvr_kv4_read(k_codes, k_scales, v_codes, v_scales, k_out, k_sb, k_st, v_out, v_sb, v_st, starts,
+                                  B, H, d, capacity, first, n, stream)
+
+
+def kv4_attn_workspace(B: int, H: int, Hkv: int, Nq: int, d: int, cache_len: int, chunk_len: int,
+                       window_chunks: int = -1) -> int:
+    """Bytes of device memory that a kv4_attn call of these sizes needs as its workspace."""
+    n = _i64(0)
+    _check(load().fastvr_kv4_attn_workspace(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks, ctypes.byref(n)))
+    return n.value
+
+
+def kv4_attn_raw(q, q_sb, q_st, k_codes, k_scales, v_codes, v_scales, o, o_sb, o_st, o_bf16, lse, workspace,
+                 workspace_bytes, lens, B, H, Hkv, Nq, d, capacity, cache_len, chunk_len, window_chunks, scale,
+                 stream=0) -> int:
+    return load().fastvr_kv4_attn(q, q_sb, q_st, k_codes, k_scales, v_codes, v_scales, o, o_sb, o_st, o_bf16, lse,
+                                  workspace, workspace_bytes, lens, B, H, Hkv, Nq, d, capacity, cache_len, chunk_len,
+                                  window_chunks, scale, stream)
 
 
 # ---------------------------------------------------------------------------
@@ -429,3 +478,304 @@ def tile_blend(tiles, Hg: int, Wg: int, *, tile: int = 64, overlap: int = 16, z_
         _check(tile_blend_update_raw(tiles.data_ptr(), z_lq.data_ptr(), out.data_ptr(), sigma, B, T, Hg, Wg, C, tile,
                                      overlap, st))
     return out
+
+
+# ---------------------------------------------------------------------------
+# rotary positions
+# ---------------------------------------------------------------------------
+
+def _view_strides(t, name):
+    """_bnhd_strides with the strides of axes of one element, which torch leaves to
+    chance, as if the view were contiguous there."""
+    B, N, H, d = t.shape
+    sb, st, sh, sd = t.stride()
+    if sd != 1 and d != 1 or sh != d and H != 1:
+        raise ValueError(f"{name}: heads and head_dim must be contiguous (stride(2) == d, stride(3) == 1)")
+    if N == 1:
+        st = H * d
+    if B == 1:
+        sb = N * st
+    return sb, st
+
+
+def _check_view(t, name, shape, dtypes):
+    if t.dtype not in dtypes or not t.is_cuda:
+        raise ValueError(f"{name} must be a {' or '.join(str(x).split('.')[1] for x in dtypes)} GPU tensor")
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    return _view_strides(t, name)
+
+
+def _check_device(ref, **tensors):
+    """Every tensor on ref's device, and that the current one: its stream takes the call."""
+    import torch
+    if ref.device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {ref.device}, the current device is cuda:{torch.cuda.current_device()}")
+    for name, t in tensors.items():
+        if t is not None and t.device != ref.device:
+            raise ValueError(f"{name} is on {t.device}, not on {ref.device}")
+
+
+def rope_inv_freq(n_pairs: int, *, base: float = 10000.0, sections=None, scaling: str | None = None,
+                  factor: float = 1.0, original_len: int = 0, fast: float = 32.0, slow: float = 1.0):
+    """(radians per position of each pair, amplitude) for ``rope``, as a list of floats and a float.
+
+    Pair j of n turns by base^(-j / n) a position.  With ``sections`` (pairs per axis,
+    for positions of several axes) each axis has frequencies of its own, j and n
+    counted within it.  ``scaling``, for contexts ``factor`` times as long as the
+    ``original_len`` positions that a model was trained on (one axis):
+
+    * ``"linear"``: every frequency divided by ``factor``;
+    * ``"ntk"``: base * factor^(n / (n - 1)), which keeps the fastest pair and divides the slowest by ``factor``;
+    * ``"yarn"`` (arXiv 2309.00071): pairs that turn ``fast`` times or more within original_len
+      are kept, those that turn ``slow`` times or less divided by ``factor``, the ones between
+      blended linearly in their turns; amplitude 0.1 ln(factor) + 1."""
+    if n_pairs < 0 or not base > 0 or not factor > 0:
+        raise ValueError("need n_pairs >= 0, base > 0 and factor > 0")
+    if sections is not None:
+        if scaling is not None:
+            raise ValueError("scaling is for positions of one axis")
+        if sum(sections) != n_pairs or min(sections) < 0:
+            raise ValueError(f"sections {tuple(sections)} do not add up to {n_pairs} pairs")
+        return [base ** (-j / n) for n in sections for j in range(n)], 1.0
+    if scaling not in (None, "linear", "ntk", "yarn"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if scaling == "ntk":
+        base *= factor ** (n_pairs / max(1, n_pairs - 1))
+    freq = [base ** (-j / n_pairs) for j in range(n_pairs)]
+    if scaling == "linear":
+        return [f / factor for f in freq], 1.0
+    if scaling == "yarn":
+        if original_len < 1 or not fast > slow:
+            raise ValueError("yarn needs original_len >= 1 and fast > slow")
+        keep = [min(1.0, max(0.0, (original_len * f / (2 * math.pi) - slow) / (fast - slow))) for f in freq]
+        return [f * k + f / factor * (1 - k) for f, k in zip(freq, keep)], 0.1 * math.log(factor) + 1.0
+    return freq, 1.0
+
+
+def _rope(x, positions, inv_freq, layout, sections, amplitude, out, out_dtype, inverse, stream):
+    import torch
+    bf16, fp32 = torch.bfloat16, torch.float32
+    if x.dim() != 4:
+        raise ValueError("x must be 4-D [B, N, H, d]")
+    shape = x.shape
+    B, N, H, d = shape
+    xs = _check_view(x, "x", shape, (bf16, fp32))
+    if layout not in ("interleaved", "half"):
+        raise ValueError(f"layout must be 'interleaved' or 'half', got {layout!r}")
+    if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be a contiguous float64 tensor [pairs]")
+    n_pairs = inv_freq.shape[0]
+    sections = (n_pairs,) if sections is None else tuple(sections)
+    A = len(sections)
+    if not 1 <= A <= 3 or sum(sections) != n_pairs or min(sections) < 0:
+        raise ValueError(f"sections {sections} must be one to three numbers of pairs that add up to {n_pairs}")
+    if positions.dtype != torch.int32 or not positions.is_contiguous():
+        raise ValueError("positions must be a contiguous int32 tensor")
+    ps = tuple(positions.shape)
+    if ps == (N, A) or A == 1 and ps == (N,):
+        pos_sb = 0
+    elif ps == (B, N, A) or A == 1 and ps == (B, N):
+        pos_sb = N * A
+    else:
+        raise ValueError(f"positions must be [N, {A}] or [B, N, {A}], got {list(ps)}")
+    if out_dtype is None:
+        out_dtype = out.dtype if out is not None else x.dtype
+    if out_dtype not in (bf16, fp32):
+        raise ValueError("out_dtype must be float32 or bfloat16")
+    if out is None:
+        out = x.new_empty(shape, dtype=out_dtype)
+        ys = (N * H * d, H * d)
+    else:
+        ys = _check_view(out, "out", shape, (out_dtype,))
+    _check_device(x, positions=positions, inv_freq=inv_freq, out=out)
+    status = load().fastvr_rope(x.data_ptr(), *xs, 1 if x.dtype == fp32 else 0, out.data_ptr(), *ys,
+                                1 if out_dtype == fp32 else 0, positions.data_ptr(), pos_sb, A, sections[0],
+                                n_pairs if A < 3 else sections[0] + sections[1], inv_freq.data_ptr(), n_pairs,
+                                amplitude, 1 if layout == "interleaved" else 0, inverse, B, N, H, d,
+                                _stream_handle(stream))
+    if status:
+        _check(status)
+    return out
+
+
+def rope(x, positions, inv_freq, *, layout: str = "interleaved", sections=None, amplitude: float = 1.0, out=None,
+         out_dtype=None, stream=None):
+    """Rotary positions of the heads x [B, N, H, d] (bf16 or fp32; views as in chunk_attn, so
+    q and k of a packed projection take one call).
+
+    ``inv_freq`` (float64 GPU tensor [pairs]) holds each pair's radians per position: the
+    first 2 * pairs elements of a head turn, the others pass.  Pairs are neighbours (``layout="interleaved"``)
+    or elements p and pairs + p (``"half"``).  ``positions`` (int32, [N, axes] or [B, N, axes]; [N]
+    or [B, N] for one axis) are the tokens' positions; with ``sections`` (up to three numbers of
+    pairs) the first section turns with axis 0, the next with axis 1 and so on: frame, row
+    and column of a video token.  The result has x's dtype unless ``out`` or ``out_dtype`` says otherwise;
+    ``out`` may be x itself."""
+    return _rope(x, positions, inv_freq, layout, sections, amplitude, out, out_dtype, 0, stream)
+
+
+def rope_bwd(dy, positions, inv_freq, *, layout: str = "interleaved", sections=None, amplitude: float = 1.0, out=None,
+             out_dtype=None, stream=None):
+    """Gradient of ``rope`` with respect to x, for the upstream gradient ``dy``: the turn by the
+    negative angles.  Arguments as in ``rope``; dq and dk of chunk_attn_bwd (fp32) go in as they are."""
+    return _rope(dy, positions, inv_freq, layout, sections, amplitude, out, out_dtype, 1, stream)
+
+
+# ---------------------------------------------------------------------------
+# KV cache in 4 bits
+# ---------------------------------------------------------------------------
+
+class KV4Cache(NamedTuple):
+    """A KV cache in 4 bits: codes [B, H, capacity, d / 2] and scales [B, H, capacity, d / 32] (uint8)
+    of keys and values; 0.53 bytes an element (the format is in include/fastvr.h)."""
+    k_codes: object
+    k_scales: object
+    v_codes: object
+    v_scales: object
+
+
+def kv4_cache(B: int, capacity: int, H: int, d: int, device="cuda") -> KV4Cache:
+    """An empty cache (zeros)."""
+    import torch
+    return KV4Cache(*(torch.zeros((B, H, capacity, n), dtype=torch.uint8, device=device)
+                      for n in (d // 2, d // 32, d // 2, d // 32)))
+
+
+def _check_kv4(cache):
+    """(B, H, capacity, d) of a cache."""
+    import torch
+    u8 = torch.uint8
+    kc, ks, vc, vs = cache
+    for t in cache:
+        if t.dtype != u8 or not t.is_cuda or not t.is_contiguous():
+            raise ValueError("a 4-bit cache is four contiguous uint8 GPU tensors")
+    shape = kc.shape
+    if len(shape) != 4:
+        raise ValueError("cache codes must be [B, H, capacity, d / 2]")
+    B, H, cap, half = shape
+    scales = (B, H, cap, half // 16)
+    if vc.shape != shape or ks.shape != scales or vs.shape != scales:
+        raise ValueError("cache shape mismatch: codes [B, H, capacity, d / 2], scales [B, H, capacity, d / 32]")
+    return B, H, cap, 2 * half
+
+
+def _check_int32(t, name, n):
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 GPU tensor [{n}]")
+    return t.data_ptr()
+
+
+def kv4_append(cache, k_new, v_new, cache_len: int = 0, *, starts=None, stream=None):
+    """Quantise k_new/v_new [B, n_new, H, d] (bf16 views) into token rows cache_len .. of the
+    cache and return the new cache length.  With ``starts`` (int32 GPU tensor [B]) sequence b's rows
+    start at starts[b] instead, rows outside the cache are dropped, and None is returned."""
+    import torch
+    B, H, cap, d = _check_kv4(cache)
+    if k_new.dim() != 4:
+        raise ValueError("k_new must be 4-D [B, n_new, H, d]")
+    n = k_new.shape[1]
+    shape = (B, n, H, d)
+    ks = _check_view(k_new, "k_new", shape, (torch.bfloat16,))
+    vs = _check_view(v_new, "v_new", shape, (torch.bfloat16,))
+    sp = _check_int32(starts, "starts", B)
+    _check_device(k_new, cache=cache[0], k_scales=cache[1], v_codes=cache[2], v_scales=cache[3], v_new=v_new,
+                  starts=starts)
+    status = load().fastvr_kv4_append(*(t.data_ptr() for t in cache), k_new.data_ptr(), *ks, v_new.data_ptr(), *vs, sp,
+                                      B, H, d, cap, cache_len, n, _stream_handle(stream))
+    if status:
+        _check(status)
+    return cache_len + n if starts is None else None
+
+
+def kv4_read(cache, n: int, first: int = 0, *, starts=None, k_out=None, v_out=None, stream=None):
+    """The values (k, v), bf16 [B, n, H, d], that the cache holds for n token rows from ``first``
+    on, or from starts[b] (int32 GPU tensor [B]) of each sequence b; rows outside the cache are then zero."""
+    import torch
+    B, H, cap, d = _check_kv4(cache)
+    shape = (B, n, H, d)
+    contiguous = (n * H * d, H * d)
+    ks = vs = contiguous
+    if k_out is None:
+        k_out = cache[0].new_empty(shape, dtype=torch.bfloat16)
+    else:
+        ks = _check_view(k_out, "k_out", shape, (torch.bfloat16,))
+    if v_out is None:
+        v_out = cache[0].new_empty(shape, dtype=torch.bfloat16)
+    else:
+        vs = _check_view(v_out, "v_out", shape, (torch.bfloat16,))
+    sp = _check_int32(starts, "starts", B)
+    _check_device(cache[0], k_scales=cache[1], v_codes=cache[2], v_scales=cache[3], k_out=k_out, v_out=v_out,
+                  starts=starts)
+    status = load().fastvr_kv4_read(*(t.data_ptr() for t in cache), k_out.data_ptr(), *ks, v_out.data_ptr(), *vs, sp, B,
+                                    H, d, cap, first, n, _stream_handle(stream))
+    if status:
+        _check(status)
+    return k_out, v_out
+
+
+# a pure function of integers; typed, so that what it refuses stays refused
+_kv4_workspace = functools.lru_cache(maxsize=256, typed=True)(kv4_attn_workspace)
+
+
+def kv4_attn(q, cache, cache_len: int, *, lens=None, chunk_len: int | None = None, window_chunks: int = -1,
+             scale: float | None = None, out=None, out_dtype=None, lse=None, return_lse: bool = True, workspace=None,
+             stream=None):
+    """Attention of the newest Nq tokens, q [B, Nq, H, d] (bf16 view), over a 4-bit cache whose
+    sequences hold cache_len tokens each, or lens[b] (int32 GPU tensor [B], at most cache_len).
+
+    Row i is the token at position length - Nq + i and sees the chunks of chunk_len tokens
+    up to its own one, window_chunks of them before it (-1: all); chunk_len None: the whole
+    cache, 1: the tokens up to its own.  H may be a multiple of the cache's heads: query head h
+    reads key head h // (H / Hkv).  Returns (o [B, Nq, H, d], float32 unless ``out`` or ``out_dtype`` says
+    bfloat16, lse fp32 [B, H, Nq] or None).  Rows that see nothing: o = 0, lse = -inf.
+    ``workspace``: a uint8 GPU tensor of kv4_attn_workspace(...) bytes, allocated here if None; two calls
+    that may run at the same time need two."""
+    import torch
+    bf16, fp32 = torch.bfloat16, torch.float32
+    B, Hkv, cap, d = _check_kv4(cache)
+    if q.dim() != 4:
+        raise ValueError("q must be 4-D [B, Nq, H, d]")
+    shape = q.shape
+    _, Nq, H, _ = shape
+    if shape[0] != B or shape[3] != d:
+        raise ValueError(f"shape mismatch: q {tuple(shape)}, cache of {B} sequences and head_dim {d}")
+    qs = _check_view(q, "q", shape, (bf16,))
+    if chunk_len is None:
+        chunk_len = max(cache_len, 1)
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    if out_dtype is None:
+        out_dtype = out.dtype if out is not None else fp32
+    if out_dtype not in (bf16, fp32):
+        raise ValueError("out_dtype must be float32 or bfloat16")
+    if out is None:
+        out = q.new_empty(shape, dtype=out_dtype)
+        os_ = (Nq * H * d, H * d)
+    else:
+        os_ = _check_view(out, "out", shape, (out_dtype,))
+    if lse is not None:
+        if lse.dtype != fp32 or lse.shape != (B, H, Nq) or not lse.is_contiguous():
+            raise ValueError("lse must be a contiguous float32 [B, H, Nq] tensor")
+    elif return_lse:
+        lse = q.new_empty((B, H, Nq), dtype=fp32)
+    lp = _check_int32(lens, "lens", B)
+    n_ws = _kv4_workspace(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks)
+    if workspace is None:
+        if n_ws:
+            workspace = q.new_empty(n_ws, dtype=torch.uint8)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor")
+    else:
+        n_ws = workspace.numel()
+    _check_device(q, cache=cache[0], k_scales=cache[1], v_codes=cache[2], v_scales=cache[3], lens=lens, out=out, lse=lse,
+                  workspace=workspace)
+    status = load().fastvr_kv4_attn(q.data_ptr(), *qs, *(t.data_ptr() for t in cache), out.data_ptr(), *os_,
+                                    1 if out_dtype == bf16 else 0, lse.data_ptr() if lse is not None else None,
+                                    workspace.data_ptr() if workspace is not None else None, n_ws, lp, B, H, Hkv, Nq, d,
+                                    cap, cache_len, chunk_len, window_chunks, scale, _stream_handle(stream))
+    if status:
+        _check(status)
+    return out, lse
