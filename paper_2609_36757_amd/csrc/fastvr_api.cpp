@@ -698,7 +698,7 @@ fastvr_status kv4_sizes(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d
       !mul_ok(rows, B, &rows) || rows > (int64_t(1) << 36))
     return fail(FASTVR_ERR_UNSUPPORTED, "sizes must be below 2^31, and B * H * Nq below 2^36");
   const fastvr::Kv4Plan plan = fastvr::kv4_plan(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks);
-  if (plan.units > fastvr::kMaxKv4Units || rows > fastvr::kMaxKv4Units * 4)
+  if (plan.units > fastvr::kMaxKv4Units || (plan.n_split > 1 && rows > fastvr::kMaxKv4Units))
     return fail(FASTVR_ERR_UNSUPPORTED, "problem needs too many workgroups");
   return FASTVR_OK;
 }

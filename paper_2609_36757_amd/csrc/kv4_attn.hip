@@ -114,7 +114,7 @@ struct Step {  // what a lane loads for 32 keys
 };
 
 template <int D, int QT>
-__global__ __launch_bounds__(kThreads) void kv4_attn_kernel(const Kv4Params p) {
+__global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(const Kv4Params p) {
   constexpr int kE = D / 16;    // elements of V a lane holds per key; O^T tiles
   constexpr int kKK = D / 32;   // reduction steps of S
   constexpr int kPitch = D + 4;
@@ -179,35 +179,49 @@ __global__ __launch_bounds__(kThreads) void kv4_attn_kernel(const Kv4Params p) {
   const uint32_t kc_off = n * (D / 2) + g * (D / 8), ks_off = n * (D / 32) + (D == 128 ? g : g >> 1);
   const uint32_t vc_off = 4 * g * (D / 2) + n * (D / 32), vs_off = 4 * g * (D / 32) + n * kE / 32;
 
-  // rows behind the cache's capacity read as zero
-  auto load = [&](int st, Step<D>& s) {
-    const uint32_t k0 = (uint32_t)st * kKv4StepKeys;
+  // The step's place goes into the scalar offset (below the slab's size), the rest are
+  // lane offsets and immediates; rows behind the cache's capacity read as zero.  (Made
+  // opaque, a lane offset is not added to each immediate ahead of the loop, which
+  // takes a register per load.)
+  Step<D> s;
+  auto opaque = [](uint32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
+  };
+  auto load_k = [&](int st) {
+    const int k0 = __builtin_amdgcn_readfirstlane(st * kKv4StepKeys);
+    const uint32_t kc = opaque(kc_off), ks = opaque(ks_off);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const uint32_t off = (k0 + 16 * x) * (D / 2) + kc_off;
+      const uint32_t off = kc + 16 * x * (D / 2);
       if (D == 128) {
-        const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rkc, off, 0, 0));
+        const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rkc, off, k0 * (D / 2), 0));
 #pragma unroll
         for (int i = 0; i < kKK; ++i) s.k[x][i] = w[i];
       } else {
-        const auto w = __builtin_amdgcn_raw_buffer_load_b64(rkc, off, 0, 0);
+        const auto w = __builtin_amdgcn_raw_buffer_load_b64(rkc, off, k0 * (D / 2), 0);
 #pragma unroll
         for (int i = 0; i < kKK; ++i) s.k[x][i] = w[i];
       }
-      s.ks[x] = __builtin_amdgcn_raw_buffer_load_b8(rks, (k0 + 16 * x) * (D / 32) + ks_off, 0, 0);
+      s.ks[x] = __builtin_amdgcn_raw_buffer_load_b8(rks, ks + 16 * x * (D / 32), k0 * (D / 32), 0);
     }
+  };
+  auto load_v = [&](int st) {
+    const int k0 = __builtin_amdgcn_readfirstlane(st * kKv4StepKeys);
+    const uint32_t vc = opaque(vc_off), vs = opaque(vs_off);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t key = k0 + (i & 3) + 16 * (i >> 2);
+      const uint32_t key = (i & 3) + 16 * (i >> 2);
       if (D == 128)
-        s.v[i] = __builtin_amdgcn_raw_buffer_load_b32(rvc, key * (D / 2) + vc_off, 0, 0);
+        s.v[i] = __builtin_amdgcn_raw_buffer_load_b32(rvc, vc + key * (D / 2), k0 * (D / 2), 0);
       else
-        s.v[i] = __builtin_amdgcn_raw_buffer_load_b16(rvc, key * (D / 2) + vc_off, 0, 0);
-      s.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(rvs, key * (D / 32) + vs_off, 0, 0);
+        s.v[i] = __builtin_amdgcn_raw_buffer_load_b16(rvc, vc + key * (D / 2), k0 * (D / 2), 0);
+      s.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(rvs, vs + key * (D / 32), k0 * (D / 32), 0);
     }
   };
 
-  auto compute = [&](int st, const Step<D>& s, auto masked) {
+  // Step st; the loads of step `nx` take the place of what has been used.
+  auto compute = [&](int st, int nx, auto masked) {
     constexpr bool MASK = decltype(masked)::value;
     const int k0 = st * kKv4StepKeys;
     f32x4 sc[QT][2];
@@ -221,10 +235,12 @@ __global__ __launch_bounds__(kThreads) void kv4_attn_kernel(const Kv4Params p) {
         for (int t = 0; t < QT; ++t) sc[t][x] = mfma16(a, q[t][kk], kk == 0 ? f32x4{} : sc[t][x]);
       }
     }
-    u32x4 pf[QT];
+    load_k(nx);
+    float m[QT];
+    bool raise = false;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      float m = -kInf;
+      m[t] = -kInf;
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -233,18 +249,26 @@ __global__ __launch_bounds__(kThreads) void kv4_attn_kernel(const Kv4Params p) {
             const int key = k0 + 16 * x + 4 * g + r;
             if (key < lo[t] || key >= hi[t]) sc[t][x][r] = -kInf;
           }
-          m = __builtin_fmaxf(m, sc[t][x][r]);
+          m[t] = __builtin_fmaxf(m[t], sc[t][x][r]);
         }
-      if (__builtin_amdgcn_ballot_w64(m * p.c > mc[t] + kSlack)) {
-        // raise the reference of every row to its maximum so far (fmaxf drops the NaN of
-        // -inf * 0, and of scores)
-        const float m_new = __builtin_fmaxf(mc[t], row_max4(m) * p.c);
+      raise |= m[t] * p.c > mc[t] + kSlack;
+    }
+    if (__builtin_amdgcn_ballot_w64(raise)) {
+      // raise the reference of every row to its maximum so far (fmaxf drops the NaN of
+      // -inf * 0, and of scores)
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        const float m_new = __builtin_fmaxf(mc[t], row_max4(m[t]) * p.c);
         const float alpha = mc[t] == -kInf ? 0.f : __builtin_amdgcn_exp2f(mc[t] - m_new);
         mc[t] = m_new;
         l[t] *= alpha;
 #pragma unroll
         for (int j = 0; j < kE; ++j) acc[t][j] *= alpha;
       }
+    }
+    u32x4 pf[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
       const float nm = mc[t] == -kInf ? 0.f : -mc[t];
       bf16x8 pb;
       float sum = 0.f;
@@ -282,6 +306,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attn_kernel(const Kv4Params p) {
         w[i][kE / 2 - 1] = kv4_pair<3>(code, scale);
       }
     }
+    load_v(nx);
 #pragma unroll
     for (int j = 0; j < kE; ++j) {
       u32x4 a;
@@ -293,6 +318,7 @@ __global__ __launch_bounds__(kThreads) void kv4_attn_kernel(const Kv4Params p) {
     }
     if (MASK && __builtin_amdgcn_ballot_w64(nan_block)) {
       // this lane's O holds one 32-element block of one row: block g (head_dim 128), g / 2 (64)
+#pragma clang loop unroll(disable)
       for (int i = 0; i < kKv4StepKeys; ++i) {
         const int key = k0 + i;
         const uint32_t byte = __builtin_amdgcn_raw_buffer_load_b8(
@@ -311,18 +337,21 @@ __global__ __launch_bounds__(kThreads) void kv4_attn_kernel(const Kv4Params p) {
     const int n_steps = (hi_max + kKv4StepKeys - 1) / kKv4StepKeys - s0;
     const int begin = s0 + (int)((int64_t)n_steps * split / p.n_split);
     const int end = s0 + (int)((int64_t)n_steps * (split + 1) / p.n_split);
-    Step<D> cur, next;
     int st = begin + wave;
-    if (st < end) load(st, cur);
-    for (; st < end; st += kKv4Waves) {
-      if (st + kKv4Waves < end) load(st + kKv4Waves, next);
-      const int k0 = st * kKv4StepKeys;
-      // all rows see all keys of the step
-      if (k0 >= lo_max && k0 + kKv4StepKeys <= hi_min)
-        compute(st, cur, std::false_type{});
-      else
-        compute(st, cur, std::true_type{});
-      cur = next;
+    if (st < end) {
+      load_k(st);
+      load_v(st);
+    }
+    // steps [in_lo, in_hi): all rows see all keys
+    const int in_lo = (lo_max + kKv4StepKeys - 1) / kKv4StepKeys, in_hi = hi_min / kKv4StepKeys;
+    // (the last step loads itself once more)
+    auto next = [&](int x) { return x + kKv4Waves < end ? x + kKv4Waves : x; };
+    const int stop = in_hi < end ? in_hi : end;
+    for (int part = 0;; ++part) {
+      const int until = part == 0 && in_lo < end ? in_lo : end;
+      for (; st < until; st += kKv4Waves) compute(st, next(st), std::true_type{});
+      if (st >= end) break;
+      for (; st < stop; st += kKv4Waves) compute(st, next(st), std::false_type{});
     }
   }
 
@@ -400,44 +429,54 @@ __global__ __launch_bounds__(kThreads) void kv4_attn_kernel(const Kv4Params p) {
   }
 }
 
-// Joins the partial results of a row's splits: one wave a row, D / 64 elements a lane.
+// Joins the partial results of a row's splits, one workgroup a row: wave w takes the
+// splits w, w + 4, ...; D / 64 elements a lane.
 template <int D>
 __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
   constexpr int kE = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * kKv4Waves + (threadIdx.x >> 6);
-  if (row >= p.rows) return;
-  const float* ml = p.part + p.rows * p.n_split * D + row * p.n_split * 2;
+  __shared__ float sm[kKv4Waves][D];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t row = blockIdx.x;
+  const float* src = p.part + row * p.n_split * D + lane * kE;
+  float x[kKv4MaxSplit / kKv4Waves][kE];
+#pragma unroll
+  for (int k = 0; k < kKv4MaxSplit / kKv4Waves; ++k)
+#pragma unroll
+    for (int j = 0; j < kE; ++j)
+      x[k][j] = k * kKv4Waves + wave < p.n_split ? src[(k * kKv4Waves + wave) * D + j] : 0.f;
   // lane s holds split s (n_split <= 64)
+  const float* ml = p.part + p.rows * p.n_split * D + row * p.n_split * 2;
   const float m_s = lane < p.n_split ? ml[2 * lane] : -kInf;
   const float l_s = lane < p.n_split ? ml[2 * lane + 1] : 0.f;
   float m = m_s;
 #pragma unroll
-  for (int x = 1; x < 64; x <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, x));
+  for (int d = 1; d < 64; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
   const float f = m_s == -kInf ? (l_s == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m_s - m);
   float sum = l_s * f;
 #pragma unroll
-  for (int x = 1; x < 64; x <<= 1) sum += __shfl_xor(sum, x);
+  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
   float v[kE] = {};
-  const float* src = p.part + row * p.n_split * D + lane * kE;
-  for (int s = 0; s < p.n_split; ++s) {
-    const float w = __shfl(f, s);
 #pragma unroll
-    for (int j = 0; j < kE; ++j) v[j] += w * src[s * D + j];
+  for (int k = 0; k < kKv4MaxSplit / kKv4Waves; ++k) {
+    const float w = __shfl(f, k * kKv4Waves + wave);
+#pragma unroll
+    for (int j = 0; j < kE; ++j) v[j] += w * x[k][j];
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const int i = (int)(row % p.nq);
-  const int64_t bh = row / p.nq;
-  const int h = (int)(bh % p.H);
-  const int64_t e = bh / p.H * p.o_sb + (int64_t)i * p.o_st + h * D + lane * kE;
 #pragma unroll
-  for (int j = 0; j < kE; ++j) {
+  for (int j = 0; j < kE; ++j) sm[wave][lane * kE + j] = v[j];
+  __syncthreads();
+  const int e = threadIdx.x;
+  if (e < D) {
+    const float o = ((sm[0][e] + sm[1][e]) + (sm[2][e] + sm[3][e])) * (sum == 0.f ? 0.f : 1.f / sum);
+    const int i = (int)(row % p.nq);
+    const int64_t bh = row / p.nq;
+    const int64_t at = bh / p.H * p.o_sb + (int64_t)i * p.o_st + (int)(bh % p.H) * D + e;
     if (p.o_bf16)
-      static_cast<__bf16*>(p.o)[e + j] = (__bf16)(v[j] * inv);
+      static_cast<__bf16*>(p.o)[at] = (__bf16)o;
     else
-      static_cast<float*>(p.o)[e + j] = v[j] * inv;
+      static_cast<float*>(p.o)[at] = o;
+    if (e == 0 && p.lse != nullptr) p.lse[row] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
   }
-  if (lane == 0 && p.lse != nullptr) p.lse[row] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
 }
 
 template <int D>
@@ -450,8 +489,7 @@ hipError_t launch_t(const Kv4Params& p, const Kv4Plan& plan, hipStream_t stream)
   if (plan.n_split > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const dim3 rows((unsigned)((plan.rows + kKv4Waves - 1) / kKv4Waves));
-    hipLaunchKernelGGL(kv4_join_kernel<D>, rows, block, 0, stream, p);
+    hipLaunchKernelGGL(kv4_join_kernel<D>, dim3((unsigned)plan.rows), block, 0, stream, p);
   }
   return hipGetLastError();
 }
