@@ -29,7 +29,7 @@
 //
 // Keys a row does not see: their P is zero, and in the steps where that can happen
 // V blocks that are not finite (rows behind a sequence may hold anything) are taken
-// as zero, and NaN is put into the O of the rows that do see them.
+// as zero, and the O of the rows that do see them becomes NaN at the end.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -47,6 +47,9 @@ using namespace dev;
 constexpr int kThreads = 64 * kKv4Waves;
 constexpr float kInf = __builtin_inff();
 constexpr float kSlack = 8.f;  // log2 units a score may exceed the running reference by
+// Reference of a row that has seen no key: below all scores, and finite, so that no
+// difference of two references is NaN; such a row's sum is 0.
+constexpr float kNone = -3e38f;
 
 struct Kv4Params {
   const uint16_t* q;
@@ -110,7 +113,7 @@ struct Step {  // what a lane loads for 32 keys
   uint32_t k[2][kK];
   uint32_t ks[2];
   uint32_t v[8];
-  uint32_t vs[8];
+  uint32_t vs[8];  // scale bytes of a key: all four (head_dim 128), or this lane's
 };
 
 template <int D, int QT>
@@ -121,6 +124,10 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
   constexpr int kRows = 16 * QT;
   __shared__ __attribute__((aligned(16))) float sm_o[kKv4Waves * 16 * kPitch];
   __shared__ float sm_m[kKv4Waves * kRows], sm_l[kKv4Waves * kRows];
+  __shared__ int sm_lo[kRows], sm_n[kRows];  // first key and number of keys that a row sees
+  // four tiles: Q's operands stay in LDS, in the order the lanes read them
+  constexpr bool kQLds = QT > 2;
+  __shared__ u32x4 sm_q[kQLds ? QT * kKK * 64 : 1];
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -144,28 +151,38 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
   interval(p, len - p.nq + row0 / p.G, len, lo_min, hi_min);
   interval(p, len - p.nq + row_last / p.G, len, lo_max, hi_max);
 
-  u32x4 q[QT][kKK];
-  int lo[QT], hi[QT];
-#pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int r = row0 + t * 16 + n;
-    const bool have = r <= row_last;
-    const int i = (have ? r : row_last) / p.G;
-    const int h = hk * p.G + (have ? r : row_last) - i * p.G;
-    interval(p, len - p.nq + i, len, lo[t], hi[t]);
+  u32x4 q[kQLds ? 1 : QT][kKK];
+  auto load_q = [&](int t, u32x4(&dst)[kKK]) {
+    const int rt = row0 + t * 16 + n, r = rt <= row_last ? rt : row_last;
+    const int i = r / p.G, h = hk * p.G + r - i * p.G;
     const uint16_t* src = p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_st + h * D + g * (D / 4);
 #pragma unroll
-    for (int kk = 0; kk < kKK; ++kk) {
-      q[t][kk] = *reinterpret_cast<const u32x4*>(src + kk * 8);
-      q[t][kk] ^= p.sign;
-    }
+    for (int kk = 0; kk < kKK; ++kk) dst[kk] = *reinterpret_cast<const u32x4*>(src + kk * 8) ^ p.sign;
+  };
+  if (kQLds) {
+    static_assert(!kQLds || QT == kKv4Waves, "a wave brings one tile of Q");
+    u32x4 mine[kKK];
+    load_q(wave, mine);
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk) sm_q[(wave * kKK + kk) * 64 + lane] = mine[kk];
+  } else {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) load_q(t, q[t]);
   }
+  if (tid < kRows) {
+    const int r = row0 + tid <= row_last ? row0 + tid : row_last;
+    int lo, hi;
+    interval(p, len - p.nq + r / p.G, len, lo, hi);
+    sm_lo[tid] = lo;
+    sm_n[tid] = hi - lo;
+  }
+  __syncthreads();
 
   f32x4 acc[QT][kE];
   float mc[QT], l[QT];  // reference in log2 units, sum of this lane's keys
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
-    mc[t] = -kInf;
+    mc[t] = kNone;
     l[t] = 0.f;
 #pragma unroll
     for (int j = 0; j < kE; ++j) acc[t][j] = f32x4{};
@@ -176,8 +193,8 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
   const __amdgpu_buffer_rsrc_t rks = make_rsrc(p.k_scales + slab * (D / 32), (int64_t)p.capacity * (D / 32));
   const __amdgpu_buffer_rsrc_t rvc = make_rsrc(p.v_codes + slab * (D / 2), (int64_t)p.capacity * (D / 2));
   const __amdgpu_buffer_rsrc_t rvs = make_rsrc(p.v_scales + slab * (D / 32), (int64_t)p.capacity * (D / 32));
-  const uint32_t kc_off = n * (D / 2) + g * (D / 8), ks_off = n * (D / 32) + (D == 128 ? g : g >> 1);
-  const uint32_t vc_off = 4 * g * (D / 2) + n * (D / 32), vs_off = 4 * g * (D / 32) + n * kE / 32;
+  // a lane's codes; its scale bytes are at 1 / 16 of these offsets (16 bytes of codes a scale)
+  const uint32_t kc_off = n * (D / 2) + g * (D / 8), vc_off = 4 * g * (D / 2) + n * (D / 32);
 
   // The step's place goes into the scalar offset (below the slab's size), the rest are
   // lane offsets and immediates; rows behind the cache's capacity read as zero.  (Made
@@ -190,7 +207,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
   };
   auto load_k = [&](int st) {
     const int k0 = __builtin_amdgcn_readfirstlane(st * kKv4StepKeys);
-    const uint32_t kc = opaque(kc_off), ks = opaque(ks_off);
+    const uint32_t kc = opaque(kc_off), ks = kc >> 4;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const uint32_t off = kc + 16 * x * (D / 2);
@@ -206,36 +223,91 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
       s.ks[x] = __builtin_amdgcn_raw_buffer_load_b8(rks, ks + 16 * x * (D / 32), k0 * (D / 32), 0);
     }
   };
+  // four tiles of head_dim 128: V's scales are loaded within their step, for want of registers
+  constexpr bool kLateScales = D == 128 && QT > 2;
+  auto load_vs = [&](int st) {
+    const int k0 = __builtin_amdgcn_readfirstlane(st * kKv4StepKeys);
+    const uint32_t vs = (opaque(vc_off) >> 4) & ~15u;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {  // (4-byte aligned: a slab's scales start at 4 * its rows)
+      const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rvs, vs + 64 * x, k0 * (D / 32), 0));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s.vs[4 * x + i] = w[i];
+    }
+  };
   auto load_v = [&](int st) {
     const int k0 = __builtin_amdgcn_readfirstlane(st * kKv4StepKeys);
-    const uint32_t vc = opaque(vc_off), vs = opaque(vs_off);
+    const uint32_t vc = opaque(vc_off);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const uint32_t key = (i & 3) + 16 * (i >> 2);
-      if (D == 128)
+      if (D == 128) {
         s.v[i] = __builtin_amdgcn_raw_buffer_load_b32(rvc, vc + key * (D / 2), k0 * (D / 2), 0);
-      else
+      } else {
         s.v[i] = __builtin_amdgcn_raw_buffer_load_b16(rvc, vc + key * (D / 2), k0 * (D / 2), 0);
-      s.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(rvs, vs + key * (D / 32), k0 * (D / 32), 0);
+        s.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(rvs, (vc >> 4) + key * (D / 32), k0 * (D / 32), 0);
+      }
+    }
+    if (D == 128 && !kLateScales) load_vs(st);
+  };
+  const uint32_t vs_shift = 8 * (n >> 2);
+  auto v_byte = [&](int i) { return D == 128 ? __builtin_amdgcn_ubfe(s.vs[i], vs_shift, 8) : s.vs[i]; };
+
+  // A step in which some row does not see some key: scores to -inf, V blocks that are
+  // not finite to zero; the O of rows that see such a block becomes NaN at the end.
+  uint32_t spoilt = 0;  // a bit per tile
+  auto mask = [&](int st, f32x4(&sc)[QT][2]) {
+    const int k0 = st * kKv4StepKeys, n0 = opaque(n);
+    bool nan_block = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (v_byte(i) > 252u) {
+        nan_block = true;
+        s.vs[i] = 0x7f7f7f7fu & (D == 128 ? ~0u : 255u);
+        s.v[i] = 0u;
+      }
+    const bool any_nan = __builtin_amdgcn_ballot_w64(nan_block) != 0;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      const int lo = sm_lo[t * 16 + n0], seen = sm_n[t * 16 + n0], at = k0 + 4 * g - lo;
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          sc[t][x][i] = (uint32_t)(at + 16 * x + i) < (uint32_t)seen ? sc[t][x][i] : -kInf;
+      if (any_nan) {
+        // this lane's O of a tile is one 32-element block of one row: block g (head_dim 128), g / 2 (64)
+#pragma clang loop unroll(disable)
+        for (int key = k0; key < k0 + kKv4StepKeys; ++key) {
+          const uint32_t byte = __builtin_amdgcn_raw_buffer_load_b8(
+              rvs, (uint32_t)key * (D / 32) + (D == 128 ? g : g >> 1), 0, 0);
+          if (byte > 252u && (uint32_t)(key - lo) < (uint32_t)seen) spoilt |= 1u << t;
+        }
+      }
     }
   };
 
-  // Step st; the loads of step `nx` take the place of what has been used.
-  auto compute = [&](int st, int nx, auto masked) {
-    constexpr bool MASK = decltype(masked)::value;
-    const int k0 = st * kKv4StepKeys;
+  // Step st; the loads of step nx take the place of what has been used.
+  auto step = [&](int st, int nx, bool masked) {
+    const uint32_t q_lane = opaque(lane);  // (Q in LDS is read anew in each step)
     f32x4 sc[QT][2];
+    const float scale[2] = {kv4_scale(s.ks[0]), kv4_scale(s.ks[1])};
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float scale = kv4_scale(s.ks[x]);
+    for (int kk = 0; kk < kKK; ++kk) {
+      const u32x4 a[2] = {kv4_values(s.k[0][kk], scale[0]), kv4_values(s.k[1][kk], scale[1])};
 #pragma unroll
-      for (int kk = 0; kk < kKK; ++kk) {
-        const u32x4 a = kv4_values(s.k[x][kk], scale);
+      for (int t = 0; t < QT; ++t) {
+        const u32x4 qf = kQLds ? sm_q[(t * kKK + kk) * 64 + q_lane] : q[kQLds ? 0 : t][kk];
 #pragma unroll
-        for (int t = 0; t < QT; ++t) sc[t][x] = mfma16(a, q[t][kk], kk == 0 ? f32x4{} : sc[t][x]);
+        for (int x = 0; x < 2; ++x) sc[t][x] = mfma16(a[x], qf, kk == 0 ? f32x4{} : sc[t][x]);
       }
+      // (no more of Q in registers than the next reduction step)
+      if (kQLds && kk % 2 == 1) __builtin_amdgcn_sched_barrier(0);
     }
+    if (kLateScales) load_vs(st);
     load_k(nx);
+    if (QT > 2) __builtin_amdgcn_sched_barrier(0);
+    if (masked) mask(st, sc);
     float m[QT];
     bool raise = false;
 #pragma unroll
@@ -244,22 +316,15 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if (MASK) {
-            const int key = k0 + 16 * x + 4 * g + r;
-            if (key < lo[t] || key >= hi[t]) sc[t][x][r] = -kInf;
-          }
-          m[t] = __builtin_fmaxf(m[t], sc[t][x][r]);
-        }
+        for (int r = 0; r < 4; ++r) m[t] = __builtin_fmaxf(m[t], sc[t][x][r]);
       raise |= m[t] * p.c > mc[t] + kSlack;
     }
     if (__builtin_amdgcn_ballot_w64(raise)) {
-      // raise the reference of every row to its maximum so far (fmaxf drops the NaN of
-      // -inf * 0, and of scores)
+      // raise the reference of every row to its maximum so far (fmaxf drops NaN scores)
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
         const float m_new = __builtin_fmaxf(mc[t], row_max4(m[t]) * p.c);
-        const float alpha = mc[t] == -kInf ? 0.f : __builtin_amdgcn_exp2f(mc[t] - m_new);
+        const float alpha = __builtin_amdgcn_exp2f(mc[t] - m_new);
         mc[t] = m_new;
         l[t] *= alpha;
 #pragma unroll
@@ -269,41 +334,30 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
     u32x4 pf[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      const float nm = mc[t] == -kInf ? 0.f : -mc[t];
       bf16x8 pb;
       float sum = 0.f;
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][x][r], p.c, nm));
-          if (MASK) {
-            const int key = k0 + 16 * x + 4 * g + r;
-            e = (key < lo[t] || key >= hi[t]) ? 0.f : e;
-          }
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][x][r], p.c, -mc[t]));  // 0 where masked
           sum += e;
           pb[4 * x + r] = (__bf16)e;
         }
       l[t] += sum;
       pf[t] = __builtin_bit_cast(u32x4, pb);
     }
+    if (QT > 2) __builtin_amdgcn_sched_barrier(0);  // one phase's registers at a time
     // V: keys 4 g + (0..3) and 16 + 4 g + (0..3), elements n * kE ..
     uint32_t w[8][kE / 2];
-    bool nan_block = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      uint32_t byte = s.vs[i], code = s.v[i];
-      if (MASK && byte > 252u) {
-        nan_block = true;
-        byte = 127u;
-        code = 0u;
-      }
-      const float scale = kv4_scale(byte);
-      w[i][0] = kv4_pair<0>(code, scale);
-      w[i][1] = kv4_pair<1>(code, scale);
+      const float scale = kv4_scale(v_byte(i));
+      w[i][0] = kv4_pair<0>(s.v[i], scale);
+      w[i][1] = kv4_pair<1>(s.v[i], scale);
       if (D == 128) {
-        w[i][kE / 2 - 2] = kv4_pair<2>(code, scale);
-        w[i][kE / 2 - 1] = kv4_pair<3>(code, scale);
+        w[i][kE / 2 - 2] = kv4_pair<2>(s.v[i], scale);
+        w[i][kE / 2 - 1] = kv4_pair<3>(s.v[i], scale);
       }
     }
     load_v(nx);
@@ -316,20 +370,6 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
 #pragma unroll
       for (int t = 0; t < QT; ++t) acc[t][j] = mfma16(a, pf[t], acc[t][j]);
     }
-    if (MASK && __builtin_amdgcn_ballot_w64(nan_block)) {
-      // this lane's O holds one 32-element block of one row: block g (head_dim 128), g / 2 (64)
-#pragma clang loop unroll(disable)
-      for (int i = 0; i < kKv4StepKeys; ++i) {
-        const int key = k0 + i;
-        const uint32_t byte = __builtin_amdgcn_raw_buffer_load_b8(
-            rvs, (uint32_t)key * (D / 32) + (D == 128 ? g : g >> 1), 0, 0);
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-          if (byte > 252u && key >= lo[t] && key < hi[t])
-#pragma unroll
-            for (int j = 0; j < kE; ++j) acc[t][j] += __builtin_nanf("");
-      }
-    }
   };
 
   if (hi_max > lo_min) {
@@ -337,22 +377,15 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
     const int n_steps = (hi_max + kKv4StepKeys - 1) / kKv4StepKeys - s0;
     const int begin = s0 + (int)((int64_t)n_steps * split / p.n_split);
     const int end = s0 + (int)((int64_t)n_steps * (split + 1) / p.n_split);
+    // steps [in_lo, in_hi): all rows see all keys
+    const int in_lo = (lo_max + kKv4StepKeys - 1) / kKv4StepKeys, in_hi = hi_min / kKv4StepKeys;
     int st = begin + wave;
     if (st < end) {
       load_k(st);
       load_v(st);
     }
-    // steps [in_lo, in_hi): all rows see all keys
-    const int in_lo = (lo_max + kKv4StepKeys - 1) / kKv4StepKeys, in_hi = hi_min / kKv4StepKeys;
-    // (the last step loads itself once more)
-    auto next = [&](int x) { return x + kKv4Waves < end ? x + kKv4Waves : x; };
-    const int stop = in_hi < end ? in_hi : end;
-    for (int part = 0;; ++part) {
-      const int until = part == 0 && in_lo < end ? in_lo : end;
-      for (; st < until; st += kKv4Waves) compute(st, next(st), std::true_type{});
-      if (st >= end) break;
-      for (; st < stop; st += kKv4Waves) compute(st, next(st), std::false_type{});
-    }
+    for (; st < end; st += kKv4Waves)  // (the last step loads itself once more)
+      step(st, st + kKv4Waves < end ? st + kKv4Waves : st, st < in_lo || st >= in_hi);
   }
 
   // join the waves
@@ -368,10 +401,10 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
   for (int t = 0; t < QT; ++t) {
     __syncthreads();
     {
-      float m = -kInf;
+      float m = kNone;
 #pragma unroll
       for (int w = 0; w < kKv4Waves; ++w) m = __builtin_fmaxf(m, sm_m[w * kRows + t * 16 + n]);
-      const float f = mc[t] == -kInf ? (l[t] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(mc[t] - m);
+      const float f = (spoilt >> t & 1) ? __builtin_nanf("") : __builtin_amdgcn_exp2f(mc[t] - m);
       float* dst = sm_o + (wave * 16 + n) * kPitch;
       // element n' * kE + j of O^T row n' = 4 g + r
 #pragma unroll
@@ -385,14 +418,12 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
     const int rr = tid >> 4, e0 = (tid & 15) * kE;
     const int r = row0 + t * 16 + rr;
     if (r < p.R) {
-      float m = -kInf, sum = 0.f;
+      float m = kNone, sum = 0.f;
 #pragma unroll
       for (int w = 0; w < kKv4Waves; ++w) m = __builtin_fmaxf(m, sm_m[w * kRows + t * 16 + rr]);
 #pragma unroll
-      for (int w = 0; w < kKv4Waves; ++w) {
-        const float mw = sm_m[w * kRows + t * 16 + rr], lw = sm_l[w * kRows + t * 16 + rr];
-        sum += mw == -kInf ? lw : lw * __builtin_amdgcn_exp2f(mw - m);
-      }
+      for (int w = 0; w < kKv4Waves; ++w)
+        sum += sm_l[w * kRows + t * 16 + rr] * __builtin_amdgcn_exp2f(sm_m[w * kRows + t * 16 + rr] - m);
       float v[kE];
 #pragma unroll
       for (int j = 0; j < kE; ++j) {
@@ -446,12 +477,12 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
       x[k][j] = k * kKv4Waves + wave < p.n_split ? src[(k * kKv4Waves + wave) * D + j] : 0.f;
   // lane s holds split s (n_split <= 64)
   const float* ml = p.part + p.rows * p.n_split * D + row * p.n_split * 2;
-  const float m_s = lane < p.n_split ? ml[2 * lane] : -kInf;
+  const float m_s = lane < p.n_split ? ml[2 * lane] : kNone;
   const float l_s = lane < p.n_split ? ml[2 * lane + 1] : 0.f;
   float m = m_s;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
-  const float f = m_s == -kInf ? (l_s == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m_s - m);
+  const float f = __builtin_amdgcn_exp2f(m_s - m);
   float sum = l_s * f;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
@@ -482,7 +513,9 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
 template <int D>
 hipError_t launch_t(const Kv4Params& p, const Kv4Plan& plan, hipStream_t stream) {
   const dim3 grid((unsigned)plan.units), block(kThreads);
-  if (plan.q_tiles == 1)
+  if (plan.q_tiles == 4)
+    hipLaunchKernelGGL((kv4_attn_kernel<D, 4>), grid, block, 0, stream, p);
+  else if (plan.q_tiles == 1)
     hipLaunchKernelGGL((kv4_attn_kernel<D, 1>), grid, block, 0, stream, p);
   else
     hipLaunchKernelGGL((kv4_attn_kernel<D, 2>), grid, block, 0, stream, p);
@@ -530,7 +563,8 @@ hipError_t launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t stream) {
   p.n_split = plan.n_split;
   p.units = (int32_t)plan.units;
   p.rows = plan.rows;
-  p.c = __builtin_fabsf(a.scale) * 1.44269504088896340736f;
+  // (not 0: masked scores, -inf * c, stay -inf; 2^-126 leaves P at 1 for all others)
+  p.c = __builtin_fmaxf(__builtin_fabsf(a.scale) * 1.44269504088896340736f, 0x1p-126f);
   p.sign = a.scale < 0.f ? 0x80008000u : 0u;
   return a.d == 128 ? launch_t<128>(p, plan, stream) : launch_t<64>(p, plan, stream);
 }

@@ -9,7 +9,7 @@
 namespace fastvr {
 
 struct Kv4Plan {
-  int32_t q_tiles;    // 16-row tiles of a workgroup: 1 or 2
+  int32_t q_tiles;    // 16-row tiles of a workgroup: 1, 2 or 4
   int64_t row_tiles;  // workgroups over the rows of one (batch, key head)
   int32_t n_split;    // workgroups over the keys of one tile
   int64_t units;      // workgroups
@@ -28,7 +28,7 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
                         int64_t window) {
   Kv4Plan p{};
   const int64_t G = H / Hkv, R = nq * G;
-  p.q_tiles = R <= 16 ? 1 : 2;
+  p.q_tiles = R <= 16 ? 1 : (R <= 32 ? 2 : 4);
   const int64_t tile = 16 * p.q_tiles;
   p.row_tiles = (R + tile - 1) / tile;
   p.rows = B * H * nq;
