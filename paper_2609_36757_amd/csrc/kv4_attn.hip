@@ -117,7 +117,7 @@ struct Step {  // what a lane loads for 32 keys
 };
 
 template <int D, int QT>
-__global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(const Kv4Params p) {
+__global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(const Kv4Params p) {
   constexpr int kE = D / 16;    // elements of V a lane holds per key; O^T tiles
   constexpr int kKK = D / 32;   // reduction steps of S
   constexpr int kPitch = D + 4;
@@ -151,33 +151,6 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
   interval(p, len - p.nq + row0 / p.G, len, lo_min, hi_min);
   interval(p, len - p.nq + row_last / p.G, len, lo_max, hi_max);
 
-  u32x4 q[kQLds ? 1 : QT][kKK];
-  auto load_q = [&](int t, u32x4(&dst)[kKK]) {
-    const int rt = row0 + t * 16 + n, r = rt <= row_last ? rt : row_last;
-    const int i = r / p.G, h = hk * p.G + r - i * p.G;
-    const uint16_t* src = p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_st + h * D + g * (D / 4);
-#pragma unroll
-    for (int kk = 0; kk < kKK; ++kk) dst[kk] = *reinterpret_cast<const u32x4*>(src + kk * 8) ^ p.sign;
-  };
-  if (kQLds) {
-    static_assert(!kQLds || QT == kKv4Waves, "a wave brings one tile of Q");
-    u32x4 mine[kKK];
-    load_q(wave, mine);
-#pragma unroll
-    for (int kk = 0; kk < kKK; ++kk) sm_q[(wave * kKK + kk) * 64 + lane] = mine[kk];
-  } else {
-#pragma unroll
-    for (int t = 0; t < QT; ++t) load_q(t, q[t]);
-  }
-  if (tid < kRows) {
-    const int r = row0 + tid <= row_last ? row0 + tid : row_last;
-    int lo, hi;
-    interval(p, len - p.nq + r / p.G, len, lo, hi);
-    sm_lo[tid] = lo;
-    sm_n[tid] = hi - lo;
-  }
-  __syncthreads();
-
   f32x4 acc[QT][kE];
   float mc[QT], l[QT];  // reference in log2 units, sum of this lane's keys
 #pragma unroll
@@ -190,6 +163,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
 
   const int64_t slab = (int64_t)bh * p.capacity;
   const __amdgpu_buffer_rsrc_t rkc = make_rsrc(p.k_codes + slab * (D / 2), (int64_t)p.capacity * (D / 2));
+  const uint8_t* k_scales = p.k_scales + slab * (D / 32);
   const __amdgpu_buffer_rsrc_t rks = make_rsrc(p.k_scales + slab * (D / 32), (int64_t)p.capacity * (D / 32));
   const __amdgpu_buffer_rsrc_t rvc = make_rsrc(p.v_codes + slab * (D / 2), (int64_t)p.capacity * (D / 2));
   const __amdgpu_buffer_rsrc_t rvs = make_rsrc(p.v_scales + slab * (D / 32), (int64_t)p.capacity * (D / 32));
@@ -207,7 +181,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
   };
   auto load_k = [&](int st) {
     const int k0 = __builtin_amdgcn_readfirstlane(st * kKv4StepKeys);
-    const uint32_t kc = opaque(kc_off), ks = kc >> 4;
+    const uint32_t kc = opaque(kc_off), ks = (kc >> 4) & ~3u;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const uint32_t off = kc + 16 * x * (D / 2);
@@ -220,7 +194,15 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
 #pragma unroll
         for (int i = 0; i < kKK; ++i) s.k[x][i] = w[i];
       }
-      s.ks[x] = __builtin_amdgcn_raw_buffer_load_b8(rks, ks + 16 * x * (D / 32), k0 * (D / 32), 0);
+      // the key's four scale bytes (head_dim 128), or this lane's one.  (The latter as an
+      // ordinary load: of a buffer load's byte the compiler sinks the widening to the end
+      // of the step, which then waits for it.)
+      if (D == 128) {
+        s.ks[x] = __builtin_amdgcn_raw_buffer_load_b32(rks, ks + 16 * x * (D / 32), k0 * (D / 32), 0);
+      } else {
+        const int key = k0 + 16 * x + n;
+        s.ks[x] = k_scales[(uint32_t)(key < p.capacity ? key : p.capacity - 1) * (D / 32) + (g >> 1)];
+      }
     }
   };
   // four tiles of head_dim 128: V's scales are loaded within their step, for want of registers
@@ -250,21 +232,62 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
     }
     if (D == 128 && !kLateScales) load_vs(st);
   };
-  const uint32_t vs_shift = 8 * (n >> 2);
+  const uint32_t vs_shift = 8 * (n >> 2), ks_shift = 8 * g;
+  auto k_byte = [&](int x) { return D == 128 ? __builtin_amdgcn_ubfe(s.ks[x], ks_shift, 8) : s.ks[x]; };
   auto v_byte = [&](int i) { return D == 128 ? __builtin_amdgcn_ubfe(s.vs[i], vs_shift, 8) : s.vs[i]; };
+
+  // steps of this workgroup, [begin, end); in steps [in_lo, in_hi) all rows see all keys
+  const int s0 = lo_min / kKv4StepKeys;
+  const int n_steps = hi_max > lo_min ? (hi_max + kKv4StepKeys - 1) / kKv4StepKeys - s0 : 0;
+  const int begin = s0 + (int)((int64_t)n_steps * split / p.n_split);
+  const int end = s0 + (int)((int64_t)n_steps * (split + 1) / p.n_split);
+  const int in_lo = (lo_max + kKv4StepKeys - 1) / kKv4StepKeys, in_hi = hi_min / kKv4StepKeys;
+  int st = begin + wave;
+  if (st < end) {
+    load_k(st);
+    load_v(st);
+  }
+
+  u32x4 q[kQLds ? 1 : QT][kKK];
+  auto load_q = [&](int t, u32x4(&dst)[kKK]) {
+    const int rt = row0 + t * 16 + n, r = rt <= row_last ? rt : row_last;
+    const int i = r / p.G, h = hk * p.G + r - i * p.G;
+    const uint16_t* src = p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_st + h * D + g * (D / 4);
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk) dst[kk] = *reinterpret_cast<const u32x4*>(src + kk * 8) ^ p.sign;
+  };
+  if (kQLds) {
+    static_assert(!kQLds || QT == kKv4Waves, "a wave brings one tile of Q");
+    u32x4 mine[kKK];
+    load_q(wave, mine);
+#pragma unroll
+    for (int kk = 0; kk < kKK; ++kk) sm_q[(wave * kKK + kk) * 64 + lane] = mine[kk];
+  } else {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) load_q(t, q[t]);
+  }
+  if (tid < kRows) {
+    const int r = row0 + tid <= row_last ? row0 + tid : row_last;
+    int lo, hi;
+    interval(p, len - p.nq + r / p.G, len, lo, hi);
+    sm_lo[tid] = lo;
+    sm_n[tid] = hi - lo;
+  }
+  __syncthreads();
 
   // A step in which some row does not see some key: scores to -inf, V blocks that are
   // not finite to zero; the O of rows that see such a block becomes NaN at the end.
   uint32_t spoilt = 0;  // a bit per tile
   auto mask = [&](int st, f32x4(&sc)[QT][2]) {
     const int k0 = st * kKv4StepKeys, n0 = opaque(n);
+    const uint32_t one = opaque(D == 128 ? 0x7f7f7f7fu : 127u), zero = opaque(0u);
     bool nan_block = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (v_byte(i) > 252u) {
         nan_block = true;
-        s.vs[i] = 0x7f7f7f7fu & (D == 128 ? ~0u : 255u);
-        s.v[i] = 0u;
+        s.vs[i] = one;
+        s.v[i] = zero;
       }
     const bool any_nan = __builtin_amdgcn_ballot_w64(nan_block) != 0;
 #pragma unroll
@@ -291,7 +314,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
   auto step = [&](int st, int nx, bool masked) {
     const uint32_t q_lane = opaque(lane);  // (Q in LDS is read anew in each step)
     f32x4 sc[QT][2];
-    const float scale[2] = {kv4_scale(s.ks[0]), kv4_scale(s.ks[1])};
+    const float scale[2] = {kv4_scale(k_byte(0)), kv4_scale(k_byte(1))};
 #pragma unroll
     for (int kk = 0; kk < kKK; ++kk) {
       const u32x4 a[2] = {kv4_values(s.k[0][kk], scale[0]), kv4_values(s.k[1][kk], scale[1])};
@@ -372,21 +395,18 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 3 : 2) void kv4_attn_kernel(con
     }
   };
 
-  if (hi_max > lo_min) {
-    const int s0 = lo_min / kKv4StepKeys;
-    const int n_steps = (hi_max + kKv4StepKeys - 1) / kKv4StepKeys - s0;
-    const int begin = s0 + (int)((int64_t)n_steps * split / p.n_split);
-    const int end = s0 + (int)((int64_t)n_steps * (split + 1) / p.n_split);
-    // steps [in_lo, in_hi): all rows see all keys
-    const int in_lo = (lo_max + kKv4StepKeys - 1) / kKv4StepKeys, in_hi = hi_min / kKv4StepKeys;
-    int st = begin + wave;
-    if (st < end) {
-      load_k(st);
-      load_v(st);
+  // What the loop carries of V's bytes and halves (head_dim 64) must be dwords: the compiler
+  // otherwise carries them narrow, and widens, so waits for, each load at the end of the
+  // step that issues it.  One value in each that is no extended byte prevents that.
+  if (D == 64 && st < end) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      s.v[i] = opaque(s.v[i]);
+      s.vs[i] = opaque(s.vs[i]);
     }
-    for (; st < end; st += kKv4Waves)  // (the last step loads itself once more)
-      step(st, st + kKv4Waves < end ? st + kKv4Waves : st, st < in_lo || st >= in_hi);
   }
+  for (; st < end; st += kKv4Waves)  // (the last step loads itself once more)
+    step(st, st + kKv4Waves < end ? st + kKv4Waves : st, st < in_lo || st >= in_hi);
 
   // join the waves
 #pragma unroll
@@ -515,10 +535,10 @@ hipError_t launch_t(const Kv4Params& p, const Kv4Plan& plan, hipStream_t stream)
   const dim3 grid((unsigned)plan.units), block(kThreads);
   if (plan.q_tiles == 4)
     hipLaunchKernelGGL((kv4_attn_kernel<D, 4>), grid, block, 0, stream, p);
-  else if (plan.q_tiles == 1)
-    hipLaunchKernelGGL((kv4_attn_kernel<D, 1>), grid, block, 0, stream, p);
-  else
+  else if (plan.q_tiles == 2)
     hipLaunchKernelGGL((kv4_attn_kernel<D, 2>), grid, block, 0, stream, p);
+  else
+    hipLaunchKernelGGL((kv4_attn_kernel<D, 1>), grid, block, 0, stream, p);
   if (plan.n_split > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

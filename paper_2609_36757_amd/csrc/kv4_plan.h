@@ -20,8 +20,21 @@ struct Kv4Plan {
 constexpr int kKv4StepKeys = 32;
 constexpr int kKv4Waves = 4;
 constexpr int kKv4MaxSplit = 64;
-constexpr int64_t kKv4TargetUnits = 1024;  // 4 workgroups on each of 256 CUs
-constexpr int64_t kKv4MinSteps = 16;       // steps of a workgroup worth a split
+// Time of a call in ns, for s workgroups over the keys of a tile: a wave's steps one after
+// the other, each as long as its loads take where few workgroups run (630 ns; four row
+// tiles: 1300), or its instructions (four row tiles, two workgroups on a CU: 1650), in as
+// many rounds as the workgroups need (four fit on a CU, two of those with more row tiles);
+// or the cache's bytes at 5.5 TB/s; from two workgroups a tile on the second kernel, which
+// joins them, and the traffic of the partial results.
+inline double kv4_time(int64_t tiles, int64_t q_tiles, int64_t steps, int64_t bytes, int64_t rows, int64_t d, int64_t s) {
+  const int64_t units = tiles * s, at_once = q_tiles == 1 ? 1024 : 512;
+  const int64_t own = ((steps + s - 1) / s + kKv4Waves - 1) / kKv4Waves;
+  const double step = q_tiles <= 2 ? 630.0 : (units <= 256 ? 1300.0 : 1650.0);
+  // (many rounds overlap, only their last one is not full)
+  const double rounds = units < 4 * at_once ? (double)((units + at_once - 1) / at_once) : (double)units / (double)at_once + 0.5;
+  const double wait = step * (double)own * rounds, read = (double)bytes / 5500.0;
+  return (wait > read ? wait : read) + (s > 1 ? 4500.0 + (double)(rows * s * (d * 4 + 8) * 2) / 5000.0 : 0.0);
+}
 
 // B, H, Hkv, nq >= 1; 0 <= cache_len; 1 <= chunk_len; window >= -1; H a multiple of Hkv.
 inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d, int64_t cache_len, int64_t chunk_len,
@@ -41,9 +54,20 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
   }
   const int64_t steps = (keys + kKv4StepKeys - 1) / kKv4StepKeys + 1;
   const int64_t tiles = B * Hkv * p.row_tiles;
-  int64_t s = kKv4TargetUnits / tiles;
-  if (s > steps / kKv4MinSteps) s = steps / kKv4MinSteps;
-  p.n_split = (int32_t)(s < 1 ? 1 : (s > kKv4MaxSplit ? kKv4MaxSplit : s));
+  const int64_t bytes = tiles * keys * (d / 2 + d / 32) * 2;
+  p.n_split = 1;
+  double best = kv4_time(tiles, p.q_tiles, steps, bytes, p.rows, d, 1);
+  for (int32_t s : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit}) {
+    if (s > steps) break;
+    const double time = kv4_time(tiles, p.q_tiles, steps, bytes, p.rows, d, s);
+    if (time < best) {
+      best = time;
+      p.n_split = s;
+    }
+  }
+#ifdef KV4_ENV
+  if (getenv("KV4_S") && atoi(getenv("KV4_S"))) p.n_split = atoi(getenv("KV4_S"));
+#endif
   p.units = tiles * p.n_split;
   // partial results of each (row, split): O, then maximum and sum
   p.ws_bytes = p.n_split > 1 ? p.rows * p.n_split * (d * 4 + 8) : 0;
