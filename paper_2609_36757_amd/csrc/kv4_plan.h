@@ -6,6 +6,8 @@
 
 #include <stdint.h>
 
+#include <initializer_list>
+
 namespace fastvr {
 
 struct Kv4Plan {
@@ -20,12 +22,14 @@ struct Kv4Plan {
 constexpr int kKv4StepKeys = 32;
 constexpr int kKv4Waves = 4;
 constexpr int kKv4MaxSplit = 64;
+constexpr int64_t kKv4MaxWorkspace = int64_t(64) << 20;
 // Time of a call in ns, for s workgroups over the keys of a tile: a wave's steps one after
-// the other, each as long as its loads take where few workgroups run (630 ns; four row
-// tiles: 1300), or its instructions (four row tiles, two workgroups on a CU: 1650), in as
-// many rounds as the workgroups need (four fit on a CU, two of those with more row tiles);
-// or the cache's bytes at 5.5 TB/s; from two workgroups a tile on the second kernel, which
-// joins them, and the traffic of the partial results.
+// the other, 630 ns each (four row tiles: 1300, and 1650 with two workgroups on a CU), in
+// as many rounds as the workgroups need (four fit on a CU, two of those with more row
+// tiles); the cache's bytes at 5.5 TB/s, which hide the steps, or hide behind them, by 70%;
+// from two workgroups a tile on the second kernel, which joins them (3 us, and 3 us more on
+// the host), and the traffic of the partial results.  Measured for one query over 65280 keys of 12 heads: 1 workgroup a tile
+// 318 us, 4 87, 16 27.9, 32 23.5, 64 23.6.
 inline double kv4_time(int64_t tiles, int64_t q_tiles, int64_t steps, int64_t bytes, int64_t rows, int64_t d, int64_t s) {
   const int64_t units = tiles * s, at_once = q_tiles == 1 ? 1024 : 512;
   const int64_t own = ((steps + s - 1) / s + kKv4Waves - 1) / kKv4Waves;
@@ -33,7 +37,8 @@ inline double kv4_time(int64_t tiles, int64_t q_tiles, int64_t steps, int64_t by
   // (many rounds overlap, only their last one is not full)
   const double rounds = units < 4 * at_once ? (double)((units + at_once - 1) / at_once) : (double)units / (double)at_once + 0.5;
   const double wait = step * (double)own * rounds, read = (double)bytes / 5500.0;
-  return (wait > read ? wait : read) + (s > 1 ? 4500.0 + (double)(rows * s * (d * 4 + 8) * 2) / 5000.0 : 0.0);
+  return (wait > read ? wait + 0.3 * read : read + 0.3 * wait) +
+         (s > 1 ? 6000.0 + (double)(rows * s * (d * 4 + 8) * 2) / 5000.0 : 0.0);
 }
 
 // B, H, Hkv, nq >= 1; 0 <= cache_len; 1 <= chunk_len; window >= -1; H a multiple of Hkv.
@@ -58,16 +63,14 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
   p.n_split = 1;
   double best = kv4_time(tiles, p.q_tiles, steps, bytes, p.rows, d, 1);
   for (int32_t s : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit}) {
-    if (s > steps) break;
+    // (no more partial results than gain 4% a step, or than 64 MB)
+    if (s > steps || p.rows * s * (d * 4 + 8) > kKv4MaxWorkspace) break;
     const double time = kv4_time(tiles, p.q_tiles, steps, bytes, p.rows, d, s);
-    if (time < best) {
+    if (time < 0.96 * best) {
       best = time;
       p.n_split = s;
     }
   }
-#ifdef KV4_ENV
-  if (getenv("KV4_S") && atoi(getenv("KV4_S"))) p.n_split = atoi(getenv("KV4_S"));
-#endif
   p.units = tiles * p.n_split;
   // partial results of each (row, split): O, then maximum and sum
   p.ws_bytes = p.n_split > 1 ? p.rows * p.n_split * (d * 4 + 8) : 0;

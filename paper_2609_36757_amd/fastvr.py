@@ -484,10 +484,15 @@ def tile_blend(tiles, Hg: int, Wg: int, *, tile: int = 64, overlap: int = 16, z_
 # rotary positions
 # ---------------------------------------------------------------------------
 
+# The checks below are on the path of calls whose kernels take 3 to 10 us, so the usual
+# case is decided with few calls into torch (0.05 to 0.1 us each): contiguous tensors, one device.
+
 def _view_strides(t, name):
     """_bnhd_strides with the strides of axes of one element, which torch leaves to
     chance, as if the view were contiguous there."""
     B, N, H, d = t.shape
+    if t.is_contiguous():
+        return N * H * d, H * d
     sb, st, sh, sd = t.stride()
     if sd != 1 and d != 1 or sh != d and H != 1:
         raise ValueError(f"{name}: heads and head_dim must be contiguous (stride(2) == d, stride(3) == 1)")
@@ -506,14 +511,24 @@ def _check_view(t, name, shape, dtypes):
     return _view_strides(t, name)
 
 
-def _check_device(ref, **tensors):
-    """Every tensor on ref's device, and that the current one: its stream takes the call."""
+def _check_device(*tensors):
+    """Every tensor on the current device: its stream takes the call."""
     import torch
-    if ref.device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {ref.device}, the current device is cuda:{torch.cuda.current_device()}")
-    for name, t in tensors.items():
-        if t is not None and t.device != ref.device:
-            raise ValueError(f"{name} is on {t.device}, not on {ref.device}")
+    try:
+        device = torch._C._cuda_getDevice()
+    except AttributeError:
+        device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"all tensors must be on the current device, cuda:{device}; one is on {t.device}")
+
+
+def _empty(like, shape, dtype):
+    """A contiguous tensor on like's device (empty_like: 0.9 us against 1.5)."""
+    import torch
+    if like.dtype is dtype and like.shape == shape and like.is_contiguous():
+        return torch.empty_like(like)
+    return like.new_empty(shape, dtype=dtype)
 
 
 def rope_inv_freq(n_pairs: int, *, base: float = 10000.0, sections=None, scaling: str | None = None,
@@ -566,13 +581,17 @@ def _rope(x, positions, inv_freq, layout, sections, amplitude, out, out_dtype, i
     if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq must be a contiguous float64 tensor [pairs]")
     n_pairs = inv_freq.shape[0]
-    sections = (n_pairs,) if sections is None else tuple(sections)
-    A = len(sections)
-    if not 1 <= A <= 3 or sum(sections) != n_pairs or min(sections) < 0:
-        raise ValueError(f"sections {sections} must be one to three numbers of pairs that add up to {n_pairs}")
+    A, split1, split2 = 1, n_pairs, n_pairs
+    if sections is not None:
+        A = len(sections)
+        if not 1 <= A <= 3 or sum(sections) != n_pairs or min(sections) < 0:
+            raise ValueError(f"sections {sections} must be one to three numbers of pairs that add up to {n_pairs}")
+        split1 = sections[0]
+        if A == 3:
+            split2 = split1 + sections[1]
     if positions.dtype != torch.int32 or not positions.is_contiguous():
         raise ValueError("positions must be a contiguous int32 tensor")
-    ps = tuple(positions.shape)
+    ps = positions.shape
     if ps == (N, A) or A == 1 and ps == (N,):
         pos_sb = 0
     elif ps == (B, N, A) or A == 1 and ps == (B, N):
@@ -583,16 +602,15 @@ def _rope(x, positions, inv_freq, layout, sections, amplitude, out, out_dtype, i
         out_dtype = out.dtype if out is not None else x.dtype
     if out_dtype not in (bf16, fp32):
         raise ValueError("out_dtype must be float32 or bfloat16")
+    ys = (N * H * d, H * d)
     if out is None:
-        out = x.new_empty(shape, dtype=out_dtype)
-        ys = (N * H * d, H * d)
+        out = _empty(x, shape, out_dtype)
     else:
         ys = _check_view(out, "out", shape, (out_dtype,))
-    _check_device(x, positions=positions, inv_freq=inv_freq, out=out)
+    _check_device(x, positions, inv_freq, out)
     status = load().fastvr_rope(x.data_ptr(), *xs, 1 if x.dtype == fp32 else 0, out.data_ptr(), *ys,
-                                1 if out_dtype == fp32 else 0, positions.data_ptr(), pos_sb, A, sections[0],
-                                n_pairs if A < 3 else sections[0] + sections[1], inv_freq.data_ptr(), n_pairs,
-                                amplitude, 1 if layout == "interleaved" else 0, inverse, B, N, H, d,
+                                1 if out_dtype == fp32 else 0, positions.data_ptr(), pos_sb, A, split1,
+                                split2, inv_freq.data_ptr(), n_pairs, amplitude, 1 if layout == "interleaved" else 0, inverse, B, N, H, d,
                                 _stream_handle(stream))
     if status:
         _check(status)
@@ -647,7 +665,7 @@ def _check_kv4(cache):
     u8 = torch.uint8
     kc, ks, vc, vs = cache
     for t in cache:
-        if t.dtype != u8 or not t.is_cuda or not t.is_contiguous():
+        if t.dtype is not u8 or not t.is_contiguous() or not t.is_cuda:
             raise ValueError("a 4-bit cache is four contiguous uint8 GPU tensors")
     shape = kc.shape
     if len(shape) != 4:
@@ -681,8 +699,7 @@ def kv4_append(cache, k_new, v_new, cache_len: int = 0, *, starts=None, stream=N
     ks = _check_view(k_new, "k_new", shape, (torch.bfloat16,))
     vs = _check_view(v_new, "v_new", shape, (torch.bfloat16,))
     sp = _check_int32(starts, "starts", B)
-    _check_device(k_new, cache=cache[0], k_scales=cache[1], v_codes=cache[2], v_scales=cache[3], v_new=v_new,
-                  starts=starts)
+    _check_device(k_new, v_new, *cache, starts)
     status = load().fastvr_kv4_append(*(t.data_ptr() for t in cache), k_new.data_ptr(), *ks, v_new.data_ptr(), *vs, sp,
                                       B, H, d, cap, cache_len, n, _stream_handle(stream))
     if status:
@@ -703,12 +720,11 @@ def kv4_read(cache, n: int, first: int = 0, *, starts=None, k_out=None, v_out=No
     else:
         ks = _check_view(k_out, "k_out", shape, (torch.bfloat16,))
     if v_out is None:
-        v_out = cache[0].new_empty(shape, dtype=torch.bfloat16)
+        v_out = _empty(k_out, shape, torch.bfloat16)
     else:
         vs = _check_view(v_out, "v_out", shape, (torch.bfloat16,))
     sp = _check_int32(starts, "starts", B)
-    _check_device(cache[0], k_scales=cache[1], v_codes=cache[2], v_scales=cache[3], k_out=k_out, v_out=v_out,
-                  starts=starts)
+    _check_device(k_out, v_out, *cache, starts)
     status = load().fastvr_kv4_read(*(t.data_ptr() for t in cache), k_out.data_ptr(), *ks, v_out.data_ptr(), *vs, sp, B,
                                     H, d, cap, first, n, _stream_handle(stream))
     if status:
@@ -751,9 +767,9 @@ def kv4_attn(q, cache, cache_len: int, *, lens=None, chunk_len: int | None = Non
         out_dtype = out.dtype if out is not None else fp32
     if out_dtype not in (bf16, fp32):
         raise ValueError("out_dtype must be float32 or bfloat16")
+    os_ = (Nq * H * d, H * d)
     if out is None:
-        out = q.new_empty(shape, dtype=out_dtype)
-        os_ = (Nq * H * d, H * d)
+        out = _empty(q, shape, out_dtype)
     else:
         os_ = _check_view(out, "out", shape, (out_dtype,))
     if lse is not None:
@@ -770,8 +786,7 @@ def kv4_attn(q, cache, cache_len: int, *, lens=None, chunk_len: int | None = Non
         raise ValueError("workspace must be a contiguous uint8 tensor")
     else:
         n_ws = workspace.numel()
-    _check_device(q, cache=cache[0], k_scales=cache[1], v_codes=cache[2], v_scales=cache[3], lens=lens, out=out, lse=lse,
-                  workspace=workspace)
+    _check_device(q, *cache, lens, out, lse, workspace)
     status = load().fastvr_kv4_attn(q.data_ptr(), *qs, *(t.data_ptr() for t in cache), out.data_ptr(), *os_,
                                     1 if out_dtype == bf16 else 0, lse.data_ptr() if lse is not None else None,
                                     workspace.data_ptr() if workspace is not None else None, n_ws, lp, B, H, Hkv, Nq, d,
