@@ -290,8 +290,8 @@ fastvr_status fastvr_tile_blend_update(const float* v_tiles, const void* z_lq, f
  *   (a, b)  ->  amplitude * (a cos - b sin, a sin + b cos)
  * with (a, b) = elements (2p, 2p + 1) when interleaved, (p, p + n_pairs)
  * otherwise.  inverse = 1 turns by the negative angle, with the same amplitude: the
- * gradient of the call with inverse = 0.  Angles are taken in fp64 (positions up
- * to 2^31 keep their fraction of a turn), the products in fp32.
+ * gradient of the call with inverse = 0.  Angles are taken in fp64 (and must stay
+ * below 2^51 radians), the products in fp32.
  *
  *   x          bf16 (x_fp32 = 0) or fp32 [B, N, H, d] view   input
  *   y          bf16 (y_fp32 = 0) or fp32 [B, N, H, d] view   output, fully overwritten
@@ -302,7 +302,7 @@ fastvr_status fastvr_tile_blend_update(const float* v_tiles, const void* z_lq, f
  * exist own no pairs: split1 = n_pairs for one axis, split2 = n_pairs for two.
  *
  * Preconditions (else FASTVR_ERR_INVALID_ARGUMENT unless noted): sizes >= 0; d in
- * {64, 128}, B <= 65535 and N * H * d < 2^33 (else FASTVR_ERR_UNSUPPORTED);
+ * {64, 128}, B and H <= 65535, N <= 2^24 (else FASTVR_ERR_UNSUPPORTED);
  * 0 <= n_pairs <= d / 2; 1 <= n_axes <= 3; 0 <= split1 <= split2 <= n_pairs as above;
  * view rules of fastvr_chunk_attn_fwd_ex for x and y; positions 4-byte and
  * inv_freq 8-byte aligned, non-NULL (inv_freq may be NULL when n_pairs = 0);

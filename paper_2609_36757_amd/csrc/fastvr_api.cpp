@@ -731,10 +731,10 @@ fastvr_status fastvr_rope(const void* x, int64_t x_sb, int64_t x_st, int32_t x_f
   if (!std::isfinite(amplitude) || !std::isfinite(static_cast<float>(amplitude)))
     return fail(FASTVR_ERR_INVALID_ARGUMENT, "amplitude is not finite");
   if (B == 0 || N == 0 || H == 0) return ok();
-  int64_t hd, size;
-  if (!mul_ok(H, d, &hd) || !mul_ok(N, hd, &size)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "size overflows int64");
-  if (B > 65535 || size >= (int64_t(1) << 33))
-    return fail(FASTVR_ERR_UNSUPPORTED, "B > 65535 or N * H * d >= 2^33");
+  // the launch grid: tokens, heads, batches
+  if (B > 65535 || H > 65535 || N > (int64_t(1) << 24))
+    return fail(FASTVR_ERR_UNSUPPORTED, "B > 65535, H > 65535 or N > 2^24");
+  const int64_t hd = H * d;
   int64_t xb, yb, pb, fb;
   fastvr_status s;
   if ((s = check_view({"x", x, x_sb, x_st, N, x_fp32 ? 4 : 2}, B, hd, &xb)) != FASTVR_OK) return s;

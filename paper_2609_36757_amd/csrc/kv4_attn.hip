@@ -98,15 +98,6 @@ __device__ __forceinline__ float row_sum4(float x) {
   return x + o;
 }
 
-// Keys [lo, hi) that the token at `pos` sees, of len.
-__device__ __forceinline__ void interval(const Kv4Params& p, int pos, int len, int& lo, int& hi) {
-  lo = hi = 0;
-  if (pos < 0) return;
-  const int c = pos / p.chunk_len, first = c * p.chunk_len;
-  lo = (p.window >= 0 && c > p.window) ? first - p.window * p.chunk_len : 0;
-  hi = len - first > p.chunk_len ? first + p.chunk_len : len;
-}
-
 template <int D>
 struct Step {  // what a lane loads for 32 keys
   static constexpr int kK = D / 32;   // dwords of K a lane holds per key
@@ -148,8 +139,8 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   const int row0 = tile * kRows;
   const int row_last = (row0 + kRows < p.R ? row0 + kRows : p.R) - 1;
   int lo_min, hi_min, lo_max, hi_max;
-  interval(p, len - p.nq + row0 / p.G, len, lo_min, hi_min);
-  interval(p, len - p.nq + row_last / p.G, len, lo_max, hi_max);
+  kv4_interval(len - p.nq + row0 / p.G, len, p.chunk_len, p.window, &lo_min, &hi_min);
+  kv4_interval(len - p.nq + row_last / p.G, len, p.chunk_len, p.window, &lo_max, &hi_max);
 
   f32x4 acc[QT][kE];
   float mc[QT], l[QT];  // reference in log2 units, sum of this lane's keys
@@ -239,8 +230,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   // steps of this workgroup, [begin, end); in steps [in_lo, in_hi) all rows see all keys
   const int s0 = lo_min / kKv4StepKeys;
   const int n_steps = hi_max > lo_min ? (hi_max + kKv4StepKeys - 1) / kKv4StepKeys - s0 : 0;
-  const int begin = s0 + (int)((int64_t)n_steps * split / p.n_split);
-  const int end = s0 + (int)((int64_t)n_steps * (split + 1) / p.n_split);
+  const int begin = s0 + kv4_split_at(n_steps, split, p.n_split), end = s0 + kv4_split_at(n_steps, split + 1, p.n_split);
   const int in_lo = (lo_max + kKv4StepKeys - 1) / kKv4StepKeys, in_hi = hi_min / kKv4StepKeys;
   int st = begin + wave;
   if (st < end) {
@@ -269,7 +259,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   if (tid < kRows) {
     const int r = row0 + tid <= row_last ? row0 + tid : row_last;
     int lo, hi;
-    interval(p, len - p.nq + r / p.G, len, lo, hi);
+    kv4_interval(len - p.nq + r / p.G, len, p.chunk_len, p.window, &lo, &hi);
     sm_lo[tid] = lo;
     sm_n[tid] = hi - lo;
   }

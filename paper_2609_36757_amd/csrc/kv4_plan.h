@@ -23,6 +23,20 @@ constexpr int kKv4StepKeys = 32;
 constexpr int kKv4Waves = 4;
 constexpr int kKv4MaxSplit = 64;
 constexpr int64_t kKv4MaxWorkspace = int64_t(64) << 20;
+// Keys [lo, hi) that the token at position pos of a sequence of len tokens sees; none
+// for pos < 0.  Neither end falls as pos grows.  (Kernel code; constexpr compiles it for
+// the host as well.)
+constexpr void kv4_interval(int pos, int len, int chunk_len, int window, int* lo, int* hi) {
+  *lo = *hi = 0;
+  if (pos < 0) return;
+  const int c = pos / chunk_len, first = c * chunk_len;
+  if (window >= 0 && c > window) *lo = first - window * chunk_len;
+  *hi = len - first > chunk_len ? first + chunk_len : len;
+}
+
+// First of n steps that workgroup `split` of `n_split` takes (the next one's first ends them).
+constexpr int kv4_split_at(int n, int split, int n_split) { return (int)((int64_t)n * split / n_split); }
+
 // Time of a call in ns, for s workgroups over the keys of a tile: a wave's steps one after
 // the other, 630 ns each (four row tiles: 1300, and 1650 with two workgroups on a CU), in
 // as many rounds as the workgroups need (four fit on a CU, two of those with more row
@@ -63,10 +77,10 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
   p.n_split = 1;
   double best = kv4_time(tiles, p.q_tiles, steps, bytes, p.rows, d, 1);
   for (int32_t s : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit}) {
-    // (no more partial results than gain 4% a step, or than 64 MB)
+    // (no more partial results than gain 2% a step, or than 64 MB)
     if (s > steps || p.rows * s * (d * 4 + 8) > kKv4MaxWorkspace) break;
     const double time = kv4_time(tiles, p.q_tiles, steps, bytes, p.rows, d, s);
-    if (time < 0.96 * best) {
+    if (time < 0.98 * best) {
       best = time;
       p.n_split = s;
     }

@@ -9,9 +9,9 @@
 // below 2e-9 and 5e-10).
 //
 // The kernel is bound by HBM bandwidth: x is read and y written once.  A thread
-// takes one unit of a token, 8 elements of a head (interleaved) or 8 + 8 (halves),
-// for up to kHeads heads: its sines and cosines are taken once for all of them,
-// while their loads are in flight.
+// takes one unit of a token, 8 (fp32: 4) elements of a head (interleaved) or twice as
+// many (halves), for one head or four: its sines and cosines are taken once for all of
+// them, while their loads are in flight.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -33,18 +33,19 @@ struct RopeParams {
   const double* f;
   int64_t pos_sb;
   int32_t n_axes, split1, split2, n_pairs;
-  uint32_t rows;  // tokens * head splits
-  int32_t H, splits, units, rows_per_block;
+  uint32_t N;
+  int32_t H, splits;  // a thread takes heads hs, hs + splits, ...
   float amp, sin_amp;  // sin_amp: negative for the inverse turn
 };
 
-// amplitude * (cos, sin) of pair p of the token at `pos`
-__device__ __forceinline__ void turn(const RopeParams& p, const int32_t* pos, int pair, float& c, float& s) {
-  const int axis = pair < p.split1 ? 0 : (pair < p.split2 ? 1 : 2);
-  const double t = (double)pos[axis] * (p.f[pair] * 0.63661977236758134308);  // quarter turns
-  const double n = __builtin_rint(t);
-  const float r = (float)(t - n);
-  const int quad = (int)(n - 4.0 * __builtin_rint(n * 0.25)) & 3;
+// amplitude * (cos, sin) of pair p, of frequency f, of a token at positions pos
+__device__ __forceinline__ void turn(const RopeParams& p, const double (&pos)[3], double f, int pair, float& c, float& s) {
+  const double at = pair < p.split1 ? pos[0] : (pair < p.split2 ? pos[1] : pos[2]);
+  const double t = at * (f * 0.63661977236758134308);  // quarter turns
+  // adding 1.5 * 2^52 rounds to an integer, whose low bits are the sum's
+  const double sum = t + 6755399441055744.0;
+  const uint32_t quad = (uint32_t)__builtin_bit_cast(uint64_t, sum);
+  const float r = (float)(t - (sum - 6755399441055744.0));
   const float z = r * r;
   // (pi/2)^k / k!
   float sn = __builtin_fmaf(z, 1.6044118e-4f, -4.6817541e-3f);
@@ -57,73 +58,76 @@ __device__ __forceinline__ void turn(const RopeParams& p, const int32_t* pos, in
   cs = __builtin_fmaf(cs, z, -1.2337006f);
   cs = __builtin_fmaf(cs, z, 1.0f);
   const float a = (quad & 1) ? sn : cs, b = (quad & 1) ? cs : sn;
-  c = ((quad == 1 || quad == 2) ? -a : a) * p.amp;
+  c = (((quad + 1) & 2) ? -a : a) * p.amp;
   s = ((quad & 2) ? -b : b) * p.sin_amp;
 }
 
-template <bool F32>
-struct Vec8;
-template <>
-struct Vec8<false> {
-  u32x4 v;
+__device__ __forceinline__ void positions(const RopeParams& p, int64_t b, int64_t tok, double (&pos)[3]) {
+  const int32_t* src = p.pos + b * p.pos_sb + tok * p.n_axes;
+  pos[0] = src[0];
+  pos[1] = pos[2] = 0.0;
+  if (p.n_axes > 1) pos[1] = src[1];
+  if (p.n_axes > 2) pos[2] = src[2];
+}
+
+// E elements of a head: 8 where x and y are bf16, else 4, so that the wider side takes
+// 16 bytes a lane and a wave's instruction one kilobyte in a row.
+template <bool F32, int E>
+struct Vec {
+  typedef uint32_t Raw __attribute__((ext_vector_type(E / 2)));
+  Raw v;
   __device__ __forceinline__ void load(const void* base, int64_t e) {
-    v = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + e);
+    v = *reinterpret_cast<const Raw*>(static_cast<const uint16_t*>(base) + e);
   }
-  __device__ __forceinline__ void unpack(float (&f)[8]) const {
+  __device__ __forceinline__ void unpack(float (&f)[E]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < E / 2; ++i) {
       f[2 * i] = __builtin_bit_cast(float, v[i] << 16);
       f[2 * i + 1] = __builtin_bit_cast(float, v[i] & 0xffff0000u);
     }
   }
-  static __device__ __forceinline__ void store(void* base, int64_t e, const float (&f)[8]) {
-    bf16x8 b;
+  static __device__ __forceinline__ void store(void* base, int64_t e, const float (&f)[E]) {
+    typedef __bf16 Out __attribute__((ext_vector_type(E)));
+    Out b;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = (__bf16)f[i];
-    *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(base) + e) = __builtin_bit_cast(u32x4, b);
+    for (int i = 0; i < E; ++i) b[i] = (__bf16)f[i];
+    *reinterpret_cast<Raw*>(static_cast<uint16_t*>(base) + e) = __builtin_bit_cast(Raw, b);
   }
 };
 template <>
-struct Vec8<true> {
-  f32x4 a, b;
+struct Vec<true, 4> {
+  f32x4 v;
   __device__ __forceinline__ void load(const void* base, int64_t e) {
-    const f32x4* s = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + e);
-    a = s[0];
-    b = s[1];
+    v = *reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + e);
   }
-  __device__ __forceinline__ void unpack(float (&f)[8]) const {
+  __device__ __forceinline__ void unpack(float (&f)[4]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f[i] = a[i];
-      f[4 + i] = b[i];
-    }
+    for (int i = 0; i < 4; ++i) f[i] = v[i];
   }
-  static __device__ __forceinline__ void store(void* base, int64_t e, const float (&f)[8]) {
-    f32x4* d = reinterpret_cast<f32x4*>(static_cast<float*>(base) + e);
-    d[0] = f32x4{f[0], f[1], f[2], f[3]};
-    d[1] = f32x4{f[4], f[5], f[6], f[7]};
+  static __device__ __forceinline__ void store(void* base, int64_t e, const float (&f)[4]) {
+    *reinterpret_cast<f32x4*>(static_cast<float*>(base) + e) = f32x4{f[0], f[1], f[2], f[3]};
   }
 };
 
 enum Layout { kInterleaved, kHalves };
+template <bool X32, bool Y32>
+constexpr int kUnit = X32 || Y32 ? 4 : 8;
 
-// grid: x = blocks of rows (token, head split), y = batch.  Lanes run over the units
-// of a row first, so neighbouring lanes read neighbouring bytes.
+// Block: x = unit of a head, y = head split, z = token; grid: x = token blocks, y = blocks
+// of head splits, z = batch.  Neighbouring lanes read neighbouring bytes.
 template <bool X32, bool Y32, int LAYOUT, int HEADS, int D>
 __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeParams p) {
-  const int lrow = (int)threadIdx.x / p.units, u = (int)threadIdx.x - lrow * p.units;
-  const uint32_t row = blockIdx.x * (uint32_t)p.rows_per_block + lrow;
-  if (lrow >= p.rows_per_block || row >= p.rows) return;
-  const uint32_t tok = row / (uint32_t)p.splits;
-  const int hs = (int)(row - tok * (uint32_t)p.splits);
-  const int64_t b = blockIdx.y;
+  const int u = threadIdx.x, hs = (int)(blockIdx.y * blockDim.y + threadIdx.y);
+  const uint32_t tok = blockIdx.x * blockDim.z + threadIdx.z;
+  if (tok >= p.N || hs >= p.splits) return;
+  const int64_t b = blockIdx.z;
   const int64_t xo = b * p.x_sb + (int64_t)tok * p.x_st, yo = b * p.y_sb + (int64_t)tok * p.y_st;
-  const int32_t* pos = p.pos + b * p.pos_sb + (int64_t)tok * p.n_axes;
-  // halves: units below n_pairs / 8 hold the pairs of elements e0 + i and e0 + n_pairs + i,
-  // the others 8 elements behind the pairs, which pass
-  const bool two = LAYOUT == kHalves && u < p.n_pairs / 8;
-  const int e0 = LAYOUT == kHalves && !two ? p.n_pairs + u * 8 : u * 8;
-  Vec8<X32> in[HEADS], in2[HEADS];
+  constexpr int E = kUnit<X32, Y32>;
+  // halves: units below n_pairs / E hold the pairs of elements e0 + i and e0 + n_pairs + i,
+  // the others E elements behind the pairs, which pass
+  const bool two = LAYOUT == kHalves && u < p.n_pairs / E;
+  const int e0 = LAYOUT == kHalves && !two ? p.n_pairs + u * E : u * E;
+  Vec<X32, E> in[HEADS], in2[HEADS];
 #pragma unroll
   for (int k = 0; k < HEADS; ++k) {
     const int h = hs + k * p.splits;
@@ -132,21 +136,26 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeParams p) {
       if (two) in2[k].load(p.x, xo + h * D + e0 + p.n_pairs);
     }
   }
-  constexpr int kPairs = LAYOUT == kHalves ? 8 : 4;
-  const int pair0 = LAYOUT == kHalves ? u * 8 : u * 4;
+  constexpr int kPairs = LAYOUT == kHalves ? E : E / 2;
+  const int pair0 = u * kPairs;
   float c[kPairs], s[kPairs];
+  if (pair0 < p.n_pairs) {
+    double pos[3], f[kPairs];
+    positions(p, b, tok, pos);
 #pragma unroll
-  for (int i = 0; i < kPairs; ++i)
-    if (pair0 + i < p.n_pairs) turn(p, pos, pair0 + i, c[i], s[i]);
+    for (int i = 0; i < kPairs; ++i) f[i] = p.f[pair0 + i < p.n_pairs ? pair0 + i : pair0];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) turn(p, pos, f[i], pair0 + i, c[i], s[i]);
+  }
 #pragma unroll
   for (int k = 0; k < HEADS; ++k) {
     const int h = hs + k * p.splits;
     if (h < p.H) {
-      float f[8], g[8];
+      float f[E], g[E];
       in[k].unpack(f);
       if (LAYOUT == kInterleaved) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < E / 2; ++i)
           if (pair0 + i < p.n_pairs) {
             const float a0 = f[2 * i], b0 = f[2 * i + 1];
             f[2 * i] = a0 * c[i] - b0 * s[i];
@@ -155,28 +164,26 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeParams p) {
       } else if (two) {
         in2[k].unpack(g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < E; ++i) {
           const float a0 = f[i], b0 = g[i];
           f[i] = a0 * c[i] - b0 * s[i];
           g[i] = a0 * s[i] + b0 * c[i];
         }
-        Vec8<Y32>::store(p.y, yo + h * D + e0 + p.n_pairs, g);
+        Vec<Y32, E>::store(p.y, yo + h * D + e0 + p.n_pairs, g);
       }
-      Vec8<Y32>::store(p.y, yo + h * D + e0, f);
+      Vec<Y32, E>::store(p.y, yo + h * D + e0, f);
     }
   }
 }
 
-// Halves whose second one does not start on 8 elements (n_pairs not a multiple of
-// 8): a unit is one pair, or one element behind the pairs.
+// Halves whose second one does not start on a unit (n_pairs not a multiple of its
+// elements): a unit is one pair, or one element behind the pairs.
 template <bool X32, bool Y32, int D>
 __global__ __launch_bounds__(kThreads) void rope_single_kernel(const RopeParams p) {
-  const int lrow = (int)threadIdx.x / p.units, u = (int)threadIdx.x - lrow * p.units;
-  const uint32_t row = blockIdx.x * (uint32_t)p.rows_per_block + lrow;
-  if (lrow >= p.rows_per_block || row >= p.rows) return;
-  const uint32_t tok = row / (uint32_t)p.splits;
-  const int hs = (int)(row - tok * (uint32_t)p.splits);
-  const int64_t b = blockIdx.y;
+  const int u = threadIdx.x, hs = (int)(blockIdx.y * blockDim.y + threadIdx.y);
+  const uint32_t tok = blockIdx.x * blockDim.z + threadIdx.z;
+  if (tok >= p.N || hs >= p.splits) return;
+  const int64_t b = blockIdx.z;
   const int64_t xo = b * p.x_sb + (int64_t)tok * p.x_st, yo = b * p.y_sb + (int64_t)tok * p.y_st;
   auto get = [&](int64_t e) {
     return X32 ? static_cast<const float*>(p.x)[e] : (float)static_cast<const __bf16*>(p.x)[e];
@@ -188,7 +195,11 @@ __global__ __launch_bounds__(kThreads) void rope_single_kernel(const RopeParams 
       static_cast<__bf16*>(p.y)[e] = (__bf16)v;
   };
   float c = 1.f, s = 0.f;
-  if (u < p.n_pairs) turn(p, p.pos + b * p.pos_sb + (int64_t)tok * p.n_axes, u, c, s);
+  if (u < p.n_pairs) {
+    double pos[3];
+    positions(p, b, tok, pos);
+    turn(p, pos, p.f[u], u, c, s);
+  }
   for (int h = hs; h < p.H; h += p.splits) {
     if (u < p.n_pairs) {
       const float a0 = get(xo + h * D + u), b0 = get(xo + h * D + u + p.n_pairs);
@@ -201,8 +212,7 @@ __global__ __launch_bounds__(kThreads) void rope_single_kernel(const RopeParams 
 }
 
 template <bool X32, bool Y32, int D>
-void launch_t(const RopeParams& p, int layout, int heads, dim3 grid, hipStream_t stream) {
-  const dim3 block(kThreads);
+void launch_t(const RopeParams& p, int layout, int heads, dim3 grid, dim3 block, hipStream_t stream) {
   auto run = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, p); };
   if (layout < 0)
     run(rope_single_kernel<X32, Y32, D>);
@@ -229,18 +239,20 @@ hipError_t launch_rope(const RopeArgs& a, hipStream_t stream) {
   p.amp = a.amplitude;
   p.sin_amp = a.inverse ? -a.amplitude : a.amplitude;
   const int d = (int)a.d;
-  const bool single = !a.interleaved && a.n_pairs % 8 != 0;
-  // units of a head: 8 elements each; halves: 8 pairs, then 8 elements behind them
-  p.units = single ? d - p.n_pairs : (a.interleaved ? d / 8 : (d - p.n_pairs) / 8);
-  p.rows_per_block = kThreads / p.units;
-  // one head a thread while that does not fill the chip, four from there
-  const int heads = a.B * a.N * a.H * p.units <= 256 * 2048 ? 1 : 4;
+  const int E = a.x_fp32 || a.y_fp32 ? 4 : 8;
+  const bool single = !a.interleaved && a.n_pairs % E != 0;
+  // units of a head: E elements each; halves: E pairs, then E elements behind them
+  const int units = single ? d - p.n_pairs : (a.interleaved ? d / E : (d - p.n_pairs) / E);
+  // four heads a thread, for one taking of its sines, where that leaves a wave for every SIMD
+  const int heads = a.B * a.N * a.H * units >= 4 * 65536 ? 4 : 1;
   p.splits = (int32_t)((a.H + heads - 1) / heads);
-  p.rows = (uint32_t)(a.N * p.splits);
-  const dim3 grid((unsigned)((p.rows + p.rows_per_block - 1) / p.rows_per_block), (unsigned)a.B);
+  p.N = (uint32_t)a.N;
+  const int ny = p.splits < kThreads / units ? p.splits : kThreads / units, nz = kThreads / (units * ny);
+  const dim3 block(units, ny, nz);
+  const dim3 grid((unsigned)((a.N + nz - 1) / nz), (unsigned)((p.splits + ny - 1) / ny), (unsigned)a.B);
   const int layout = single ? -1 : (a.interleaved ? kInterleaved : kHalves);
 #define FASTVR_ROPE_T(X, Y) \
-  (d == 128 ? launch_t<X, Y, 128>(p, layout, heads, grid, stream) : launch_t<X, Y, 64>(p, layout, heads, grid, stream))
+  (d == 128 ? launch_t<X, Y, 128>(p, layout, heads, grid, block, stream) : launch_t<X, Y, 64>(p, layout, heads, grid, block, stream))
   if (a.x_fp32)
     a.y_fp32 ? FASTVR_ROPE_T(true, true) : FASTVR_ROPE_T(true, false);
   else

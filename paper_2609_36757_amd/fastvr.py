@@ -609,9 +609,9 @@ def _rope(x, positions, inv_freq, layout, sections, amplitude, out, out_dtype, i
         ys = _check_view(out, "out", shape, (out_dtype,))
     _check_device(x, positions, inv_freq, out)
     status = load().fastvr_rope(x.data_ptr(), *xs, 1 if x.dtype == fp32 else 0, out.data_ptr(), *ys,
-                                1 if out_dtype == fp32 else 0, positions.data_ptr(), pos_sb, A, split1,
-                                split2, inv_freq.data_ptr(), n_pairs, amplitude, 1 if layout == "interleaved" else 0, inverse, B, N, H, d,
-                                _stream_handle(stream))
+                                1 if out_dtype == fp32 else 0, positions.data_ptr(), pos_sb, A, split1, split2,
+                                inv_freq.data_ptr(), n_pairs, amplitude, 1 if layout == "interleaved" else 0, inverse,
+                                B, N, H, d, _stream_handle(stream))
     if status:
         _check(status)
     return out
