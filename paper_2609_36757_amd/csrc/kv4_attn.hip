@@ -302,6 +302,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
 
   // Step st; the loads of step nx take the place of what has been used.
   auto step = [&](int st, int nx, bool masked) {
+    __builtin_amdgcn_s_setprio(1);
     const uint32_t q_lane = opaque(lane);  // (Q in LDS is read anew in each step)
     f32x4 sc[QT][2];
     const float scale[2] = {kv4_scale(k_byte(0)), kv4_scale(k_byte(1))};
@@ -317,6 +318,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
       // (no more of Q in registers than the next reduction step)
       if (kQLds && kk % 2 == 1) __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     if (kLateScales) load_vs(st);
     load_k(nx);
     if (QT > 2) __builtin_amdgcn_sched_barrier(0);
@@ -361,27 +363,43 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
       pf[t] = __builtin_bit_cast(u32x4, pb);
     }
     if (QT > 2) __builtin_amdgcn_sched_barrier(0);  // one phase's registers at a time
-    // V: keys 4 g + (0..3) and 16 + 4 g + (0..3), elements n * kE ..
-    uint32_t w[8][kE / 2];
+    // V: keys 4 g + (0..3) and 16 + 4 g + (0..3), elements n * kE ..; two elements of the 8
+    // keys at a time are converted and paired while the last two's products run
+    __builtin_amdgcn_s_setprio(1);
+    uint32_t code[8];
+    float v_scale[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float scale = kv4_scale(v_byte(i));
-      w[i][0] = kv4_pair<0>(s.v[i], scale);
-      w[i][1] = kv4_pair<1>(s.v[i], scale);
-      if (D == 128) {
-        w[i][kE / 2 - 2] = kv4_pair<2>(s.v[i], scale);
-        w[i][kE / 2 - 1] = kv4_pair<3>(s.v[i], scale);
-      }
+      code[i] = s.v[i];
+      v_scale[i] = kv4_scale(v_byte(i));
     }
     load_v(nx);
+    auto two = [&](auto pair) {
+      constexpr int P = decltype(pair)::value;
+      uint32_t w[8];
 #pragma unroll
-    for (int j = 0; j < kE; ++j) {
-      u32x4 a;
+      for (int i = 0; i < 8; ++i) w[i] = kv4_pair<P>(code[i], v_scale[i]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        a[i] = __builtin_amdgcn_perm(w[2 * i + 1][j / 2], w[2 * i][j / 2], (j & 1) ? 0x07060302u : 0x05040100u);
+      for (int j = 2 * P; j < 2 * P + 2; ++j) {
+        u32x4 a;
 #pragma unroll
-      for (int t = 0; t < QT; ++t) acc[t][j] = mfma16(a, pf[t], acc[t][j]);
+        for (int i = 0; i < 4; ++i)
+          a[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], (j & 1) ? 0x07060302u : 0x05040100u);
+#pragma unroll
+        for (int t = 0; t < QT; ++t) acc[t][j] = mfma16(a, pf[t], acc[t][j]);
+      }
+    };
+    two(std::integral_constant<int, 0>{});
+    two(std::integral_constant<int, 1>{});
+    if (D == 128) {
+      two(std::integral_constant<int, kE / 2 - 2>{});
+      two(std::integral_constant<int, kE / 2 - 1>{});
+    }
+    __builtin_amdgcn_sched_group_barrier(SCHED_VALU, 32, 0);
+#pragma unroll
+    for (int i = 0; i < QT * kE; ++i) {
+      __builtin_amdgcn_sched_group_barrier(SCHED_MFMA, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(SCHED_VALU, 8 / QT, 0);
     }
   };
 
