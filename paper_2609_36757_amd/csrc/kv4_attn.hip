@@ -143,10 +143,13 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   kv4_interval(len - p.nq + row_last / p.G, len, p.chunk_len, p.window, &lo_max, &hi_max);
 
   f32x4 acc[QT][kE];
-  float mc[QT], l[QT];  // reference in log2 units, sum of this lane's keys
+  // reference in log2 units, the score from which it is raised, sum of this lane's keys
+  float mc[QT], bound[QT], l[QT];
+  const float inv_c = 1.0f / p.c;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     mc[t] = kNone;
+    bound[t] = -kInf;
     l[t] = 0.f;
 #pragma unroll
     for (int j = 0; j < kE; ++j) acc[t][j] = f32x4{};
@@ -332,7 +335,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int r = 0; r < 4; ++r) m[t] = __builtin_fmaxf(m[t], sc[t][x][r]);
-      raise |= m[t] * p.c > mc[t] + kSlack;
+      raise |= m[t] > bound[t];
     }
     if (__builtin_amdgcn_ballot_w64(raise)) {
       // raise the reference of every row to its maximum so far (fmaxf drops NaN scores)
@@ -341,6 +344,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
         const float m_new = __builtin_fmaxf(mc[t], row_max4(m[t]) * p.c);
         const float alpha = __builtin_amdgcn_exp2f(mc[t] - m_new);
         mc[t] = m_new;
+        bound[t] = (m_new + kSlack) * inv_c;
         l[t] *= alpha;
 #pragma unroll
         for (int j = 0; j < kE; ++j) acc[t][j] *= alpha;
