@@ -429,22 +429,28 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
       sm_l[wave * kRows + t * 16 + n] = l[t];
     }
   }
-#pragma unroll
+  // (a loop, though tiles are picked by constants: each unrolled round's instructions would
+  // be fetched for one use, 1.1 us a round)
+#pragma clang loop unroll(disable)
   for (int t = 0; t < QT; ++t) {
     __syncthreads();
     {
       float m = kNone;
 #pragma unroll
       for (int w = 0; w < kKv4Waves; ++w) m = __builtin_fmaxf(m, sm_m[w * kRows + t * 16 + n]);
-      const float f = (spoilt >> t & 1) ? __builtin_nanf("") : __builtin_amdgcn_exp2f(mc[t] - m);
+      const float own = sm_m[wave * kRows + t * 16 + n];
+      const float f = (spoilt >> t & 1) ? __builtin_nanf("") : __builtin_amdgcn_exp2f(own - m);
       float* dst = sm_o + (wave * 16 + n) * kPitch;
       // element n' * kE + j of O^T row n' = 4 g + r
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int x = 0; x < QT; ++x)
+        if (x == t)
 #pragma unroll
-        for (int j = 0; j < kE; j += 4)
-          *reinterpret_cast<f32x4*>(dst + (4 * g + r) * kE + j) =
-              f32x4{acc[t][j][r] * f, acc[t][j + 1][r] * f, acc[t][j + 2][r] * f, acc[t][j + 3][r] * f};
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int j = 0; j < kE; j += 4)
+              *reinterpret_cast<f32x4*>(dst + (4 * g + r) * kE + j) =
+                  f32x4{acc[x][j][r] * f, acc[x][j + 1][r] * f, acc[x][j + 2][r] * f, acc[x][j + 3][r] * f};
     }
     __syncthreads();
     const int rr = tid >> 4, e0 = (tid & 15) * kE;
@@ -478,13 +484,16 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const int64_t e = (int64_t)b * p.o_sb + (int64_t)i * p.o_st + h * D + e0;
         if (p.o_bf16) {
-          __bf16* dst = static_cast<__bf16*>(p.o) + e;
+          typedef __bf16 Row __attribute__((ext_vector_type(kE)));
+          Row row;
 #pragma unroll
-          for (int j = 0; j < kE; ++j) dst[j] = (__bf16)(v[j] * inv);
+          for (int j = 0; j < kE; ++j) row[j] = (__bf16)(v[j] * inv);
+          *reinterpret_cast<Row*>(static_cast<__bf16*>(p.o) + e) = row;
         } else {
           float* dst = static_cast<float*>(p.o) + e;
 #pragma unroll
-          for (int j = 0; j < kE; ++j) dst[j] = v[j] * inv;
+          for (int j = 0; j < kE; j += 4)
+            *reinterpret_cast<f32x4*>(dst + j) = f32x4{v[j] * inv, v[j + 1] * inv, v[j + 2] * inv, v[j + 3] * inv};
         }
         if (e0 == 0 && p.lse != nullptr) p.lse[out_row] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
       }
