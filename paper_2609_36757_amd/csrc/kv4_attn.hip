@@ -501,21 +501,23 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   }
 }
 
-// Joins the partial results of a row's splits, one workgroup a row: wave w takes the
-// splits w, w + 4, ...; D / 64 elements a lane.
-template <int D>
+// Joins the partial results of a row's splits.  WAVES = 4: a workgroup a row, wave w taking
+// the splits w, w + 4, ...; WAVES = 1, for up to 16 splits: a wave a row.  D / 64 elements a lane.
+template <int D, int WAVES>
 __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
-  constexpr int kE = D / 64;
-  __shared__ float sm[kKv4Waves][D];
+  constexpr int kE = D / 64, kMine = 16;
+  static_assert(kMine * kKv4Waves == kKv4MaxSplit, "every split has a wave");
+  __shared__ float sm[WAVES == 1 ? 1 : kKv4Waves][D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row = blockIdx.x;
+  const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * kKv4Waves + wave : (int64_t)blockIdx.x;
+  if (row >= p.rows) return;  // (whole waves, and with WAVES = 4 whole workgroups)
+  const int first = WAVES == 1 ? 0 : wave;
   const float* src = p.part + row * p.n_split * D + lane * kE;
-  float x[kKv4MaxSplit / kKv4Waves][kE];
+  float x[kMine][kE];
 #pragma unroll
-  for (int k = 0; k < kKv4MaxSplit / kKv4Waves; ++k)
+  for (int k = 0; k < kMine; ++k)
 #pragma unroll
-    for (int j = 0; j < kE; ++j)
-      x[k][j] = k * kKv4Waves + wave < p.n_split ? src[(k * kKv4Waves + wave) * D + j] : 0.f;
+    for (int j = 0; j < kE; ++j) x[k][j] = k * WAVES + first < p.n_split ? src[(k * WAVES + first) * D + j] : 0.f;
   // lane s holds split s (n_split <= 64)
   const float* ml = p.part + p.rows * p.n_split * D + row * p.n_split * 2;
   const float m_s = lane < p.n_split ? ml[2 * lane] : kNone;
@@ -529,26 +531,32 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
   float v[kE] = {};
 #pragma unroll
-  for (int k = 0; k < kKv4MaxSplit / kKv4Waves; ++k) {
-    const float w = __shfl(f, k * kKv4Waves + wave);
+  for (int k = 0; k < kMine; ++k) {
+    const float w = __shfl(f, k * WAVES + first);
 #pragma unroll
     for (int j = 0; j < kE; ++j) v[j] += w * x[k][j];
   }
+  if (WAVES > 1) {
 #pragma unroll
-  for (int j = 0; j < kE; ++j) sm[wave][lane * kE + j] = v[j];
-  __syncthreads();
-  const int e = threadIdx.x;
-  if (e < D) {
-    const float o = ((sm[0][e] + sm[1][e]) + (sm[2][e] + sm[3][e])) * (sum == 0.f ? 0.f : 1.f / sum);
-    const int i = (int)(row % p.nq);
-    const int64_t bh = row / p.nq;
-    const int64_t at = bh / p.H * p.o_sb + (int64_t)i * p.o_st + (int)(bh % p.H) * D + e;
-    if (p.o_bf16)
-      static_cast<__bf16*>(p.o)[at] = (__bf16)o;
-    else
-      static_cast<float*>(p.o)[at] = o;
-    if (e == 0 && p.lse != nullptr) p.lse[row] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
+    for (int j = 0; j < kE; ++j) sm[wave][lane * kE + j] = v[j];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int j = 0; j < kE; ++j)
+      v[j] = (sm[0][lane * kE + j] + sm[1 % WAVES][lane * kE + j]) + (sm[2 % WAVES][lane * kE + j] + sm[3 % WAVES][lane * kE + j]);
   }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const int i = (int)(row % p.nq);
+  const int64_t bh = row / p.nq;
+  const int64_t e = bh / p.H * p.o_sb + (int64_t)i * p.o_st + (int)(bh % p.H) * D + lane * kE;
+#pragma unroll
+  for (int j = 0; j < kE; ++j) {
+    if (p.o_bf16)
+      static_cast<__bf16*>(p.o)[e + j] = (__bf16)(v[j] * inv);
+    else
+      static_cast<float*>(p.o)[e + j] = v[j] * inv;
+  }
+  if (lane == 0 && p.lse != nullptr) p.lse[row] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
 }
 
 template <int D>
@@ -563,7 +571,12 @@ hipError_t launch_t(const Kv4Params& p, const Kv4Plan& plan, hipStream_t stream)
   if (plan.n_split > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kv4_join_kernel<D>, dim3((unsigned)plan.rows), block, 0, stream, p);
+    // a wave a row where that fills the chip
+    if (plan.n_split <= 16 && plan.rows >= 2048)
+      hipLaunchKernelGGL((kv4_join_kernel<D, 1>), dim3((unsigned)((plan.rows + kKv4Waves - 1) / kKv4Waves)), block, 0, stream,
+                         p);
+    else
+      hipLaunchKernelGGL((kv4_join_kernel<D, 4>), dim3((unsigned)plan.rows), block, 0, stream, p);
   }
   return hipGetLastError();
 }

@@ -37,22 +37,33 @@ constexpr void kv4_interval(int pos, int len, int chunk_len, int window, int* lo
 // First of n steps that workgroup `split` of `n_split` takes (the next one's first ends them).
 constexpr int kv4_split_at(int n, int split, int n_split) { return (int)((int64_t)n * split / n_split); }
 
-// Time of a call in ns, for s workgroups over the keys of a tile: a wave's steps one after
-// the other, 630 ns each (four row tiles: 1300, and 1650 with two workgroups on a CU), in
-// as many rounds as the workgroups need (four fit on a CU, two of those with more row
-// tiles); the cache's bytes at 5.5 TB/s, which hide the steps, or hide behind them, by 70%;
-// from two workgroups a tile on the second kernel, which joins them (3 us, and 3 us more on
-// the host), and the traffic of the partial results.  Measured for one query over 65280 keys of 12 heads: 1 workgroup a tile
-// 318 us, 4 87, 16 27.9, 32 23.5, 64 23.6.
-inline double kv4_time(int64_t tiles, int64_t q_tiles, int64_t steps, int64_t bytes, int64_t rows, int64_t d, int64_t s) {
-  const int64_t units = tiles * s, at_once = q_tiles == 1 ? 1024 : 512;
+// Time of a call in ns with q row tiles a workgroup (of `tiles` such tiles) and s
+// workgroups over the keys of each, from measurements on a chip with 256 CUs:
+//  * what a workgroup needs besides its steps: 4.3, 5.5 and 8 us for 1, 2 and 4 row tiles;
+//  * a wave's steps one after the other, 630, 650 and 1080 ns each while a CU has one
+//    workgroup, 400, 600 and 830 ns a workgroup where its instructions are the limit
+//    (head_dim 64: 0.85 of that), in as many rounds as do not fit at once (4, 2 and 2 on a CU);
+//  * the cache at 5.5 TB/s once, and from L2 at four times that for every other row tile; of
+//    this and the steps the shorter hides behind the longer by 70%;
+//  * from two workgroups a tile on the second kernel, 3 us and 3 us more on the host, 0.25 ns a
+//    row, and the partial results written and read.
+// Measured, 12 heads, head_dim 128: one query over 65280 keys 318 us with 1 workgroup a tile, 87 with
+// 4, 27.9 with 16, 23.5 with 32; 64 queries over 1000 keys 9.3, 11.3 and 16.6 us with 1, 2 and 4 row
+// tiles, 3120 over 18720 keys 410 and 369 us with 2 and 4.
+inline double kv4_time(int64_t tiles, int q, int64_t steps, double bytes, int64_t rows, int64_t d, int64_t s) {
+  const int at = q == 1 ? 0 : (q == 2 ? 1 : 2);
+  constexpr double kFixed[3] = {4300, 5500, 8000}, kWait[3] = {630, 650, 1080}, kBusy[3] = {400, 600, 830};
+  constexpr int64_t kAtOnce[3] = {4 * 256, 2 * 256, 2 * 256};
+  const int64_t units = tiles * s, here = units < kAtOnce[at] ? units : kAtOnce[at];
   const int64_t own = ((steps + s - 1) / s + kKv4Waves - 1) / kKv4Waves;
-  const double step = q_tiles <= 2 ? 630.0 : (units <= 256 ? 1300.0 : 1650.0);
+  const double busy = kBusy[at] * (double)((here + 255) / 256);
+  const double step = (kWait[at] > busy ? kWait[at] : busy) * (d == 128 ? 1.0 : 0.85);
   // (many rounds overlap, only their last one is not full)
-  const double rounds = units < 4 * at_once ? (double)((units + at_once - 1) / at_once) : (double)units / (double)at_once + 0.5;
-  const double wait = step * (double)own * rounds, read = (double)bytes / 5500.0;
-  return (wait > read ? wait + 0.3 * read : read + 0.3 * wait) +
-         (s > 1 ? 6000.0 + (double)(rows * s * (d * 4 + 8) * 2) / 5000.0 : 0.0);
+  const double rounds = units < 4 * kAtOnce[at] ? (double)((units + kAtOnce[at] - 1) / kAtOnce[at])
+                                                : (double)units / (double)kAtOnce[at] + 0.5;
+  const double wait = step * (double)own * rounds, read = bytes / 5500.0;
+  return kFixed[at] + (wait > read ? wait + 0.3 * read : read + 0.3 * wait) +
+         (s > 1 ? 6000.0 + 0.25 * (double)rows + (double)(rows * s * (d * 4 + 8) * 2) / 5000.0 : 0.0);
 }
 
 // B, H, Hkv, nq >= 1; 0 <= cache_len; 1 <= chunk_len; window >= -1; H a multiple of Hkv.
@@ -60,31 +71,33 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
                         int64_t window) {
   Kv4Plan p{};
   const int64_t G = H / Hkv, R = nq * G;
-  p.q_tiles = R <= 16 ? 1 : (R <= 32 ? 2 : 4);
-  const int64_t tile = 16 * p.q_tiles;
-  p.row_tiles = (R + tile - 1) / tile;
   p.rows = B * H * nq;
-  // keys that a tile's rows see at most: their own chunks and the window before them
-  int64_t keys = cache_len;
-  const int64_t tokens = (tile + G - 1) / G + 1;
-  if (window >= 0 && chunk_len < cache_len && window < cache_len / chunk_len) {
-    const int64_t span = (window + 2) * chunk_len + tokens;
-    keys = span < keys ? span : keys;
-  }
-  const int64_t steps = (keys + kKv4StepKeys - 1) / kKv4StepKeys + 1;
-  const int64_t tiles = B * Hkv * p.row_tiles;
-  const int64_t bytes = tiles * keys * (d / 2 + d / 32) * 2;
-  p.n_split = 1;
-  double best = kv4_time(tiles, p.q_tiles, steps, bytes, p.rows, d, 1);
-  for (int32_t s : {2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit}) {
-    // (no more partial results than gain 2% a step, or than 64 MB)
-    if (s > steps || p.rows * s * (d * 4 + 8) > kKv4MaxWorkspace) break;
-    const double time = kv4_time(tiles, p.q_tiles, steps, bytes, p.rows, d, s);
-    if (time < 0.98 * best) {
-      best = time;
-      p.n_split = s;
+  double best = 0;
+  for (int q : {4, 2, 1}) {
+    if (q > 1 && R <= 8 * q) continue;  // half of the rows, and more, would be empty
+    const int64_t tile = 16 * q, row_tiles = (R + tile - 1) / tile, tiles = B * Hkv * row_tiles;
+    // keys that a tile's rows see at most: their own chunks and the window before them
+    int64_t keys = cache_len;
+    const int64_t tokens = (tile + G - 1) / G + 1;
+    if (window >= 0 && chunk_len < cache_len && window < cache_len / chunk_len) {
+      const int64_t span = (window + 2) * chunk_len + tokens;
+      keys = span < keys ? span : keys;
+    }
+    const int64_t steps = (keys + kKv4StepKeys - 1) / kKv4StepKeys + 1;
+    const double bytes = (double)(B * Hkv * keys * (d / 2 + d / 32) * 2) * (1.0 + 0.25 * (double)(row_tiles - 1));
+    for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit}) {
+      if (s > 1 && (s > steps || p.rows * s * (d * 4 + 8) > kKv4MaxWorkspace)) break;
+      const double time = kv4_time(tiles, q, steps, bytes, p.rows, d, s);
+      // (2%: no more partial results for nothing)
+      if (p.q_tiles == 0 || time < 0.98 * best) {
+        best = time;
+        p.q_tiles = q;
+        p.n_split = s;
+        p.row_tiles = row_tiles;
+      }
     }
   }
+  const int64_t tiles = B * Hkv * p.row_tiles;
   p.units = tiles * p.n_split;
   // partial results of each (row, split): O, then maximum and sum
   p.ws_bytes = p.n_split > 1 ? p.rows * p.n_split * (d * 4 + 8) : 0;
