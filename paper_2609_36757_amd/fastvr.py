@@ -503,24 +503,31 @@ def _view_strides(t, name):
     return sb, st
 
 
-def _check_view(t, name, shape, dtypes):
-    if t.dtype not in dtypes or not t.is_cuda:
-        raise ValueError(f"{name} must be a {' or '.join(str(x).split('.')[1] for x in dtypes)} GPU tensor")
+def _check_view(t, name, shape, dtype):
+    """Strides of a [B, N, H, d] view of that shape and dtype."""
+    if t.dtype is not dtype or not t.is_cuda:
+        raise ValueError(f"{name} must be a {str(dtype).split('.')[1]} GPU tensor")
     if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     return _view_strides(t, name)
 
 
-def _check_device(*tensors):
-    """Every tensor on the current device: its stream takes the call."""
+def _stream_on(device: int, stream, *tensors):
+    """Handle of the stream that takes a call on the tensors (None: not given): the given one, or the
+    current one of the current device, which all tensors have to be on."""
     import torch
     try:
-        device = torch._C._cuda_getDevice()
-    except AttributeError:
-        device = torch.cuda.current_device()
+        current = torch._C._cuda_getDevice()
+        handle = torch._C._cuda_getCurrentRawStream(current) if stream is None else stream.cuda_stream
+    except AttributeError:  # (as in _stream_handle)
+        current = torch.cuda.current_device()
+        handle = _stream_handle(stream)
+    if device != current:
+        raise ValueError(f"the tensors are on cuda:{device}, the current device is cuda:{current}")
     for t in tensors:
         if t is not None and t.get_device() != device:
-            raise ValueError(f"all tensors must be on the current device, cuda:{device}; one is on {t.device}")
+            raise ValueError(f"all tensors must be on cuda:{device}, one is on {t.device}")
+    return handle
 
 
 def _empty(like, shape, dtype):
@@ -575,10 +582,11 @@ def _rope(x, positions, inv_freq, layout, sections, amplitude, out, out_dtype, i
         raise ValueError("x must be 4-D [B, N, H, d]")
     shape = x.shape
     B, N, H, d = shape
-    xs = _check_view(x, "x", shape, (bf16, fp32))
+    x32 = x.dtype is fp32
+    xs = _check_view(x, "x", shape, fp32 if x32 else bf16)
     if layout not in ("interleaved", "half"):
         raise ValueError(f"layout must be 'interleaved' or 'half', got {layout!r}")
-    if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+    if inv_freq.dtype is not torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise ValueError("inv_freq must be a contiguous float64 tensor [pairs]")
     n_pairs = inv_freq.shape[0]
     A, split1, split2 = 1, n_pairs, n_pairs
@@ -589,7 +597,7 @@ def _rope(x, positions, inv_freq, layout, sections, amplitude, out, out_dtype, i
         split1 = sections[0]
         if A == 3:
             split2 = split1 + sections[1]
-    if positions.dtype != torch.int32 or not positions.is_contiguous():
+    if positions.dtype is not torch.int32 or not positions.is_contiguous():
         raise ValueError("positions must be a contiguous int32 tensor")
     ps = positions.shape
     if ps == (N, A) or A == 1 and ps == (N,):
@@ -600,18 +608,18 @@ def _rope(x, positions, inv_freq, layout, sections, amplitude, out, out_dtype, i
         raise ValueError(f"positions must be [N, {A}] or [B, N, {A}], got {list(ps)}")
     if out_dtype is None:
         out_dtype = out.dtype if out is not None else x.dtype
-    if out_dtype not in (bf16, fp32):
+    if out_dtype is not bf16 and out_dtype is not fp32:
         raise ValueError("out_dtype must be float32 or bfloat16")
+    handle = _stream_on(x.get_device(), stream, positions, inv_freq, out)
     ys = (N * H * d, H * d)
     if out is None:
         out = _empty(x, shape, out_dtype)
     else:
-        ys = _check_view(out, "out", shape, (out_dtype,))
-    _check_device(x, positions, inv_freq, out)
-    status = load().fastvr_rope(x.data_ptr(), *xs, 1 if x.dtype == fp32 else 0, out.data_ptr(), *ys,
-                                1 if out_dtype == fp32 else 0, positions.data_ptr(), pos_sb, A, split1, split2,
+        ys = _check_view(out, "out", shape, out_dtype)
+    status = load().fastvr_rope(x.data_ptr(), *xs, 1 if x32 else 0, out.data_ptr(), *ys,
+                                1 if out_dtype is fp32 else 0, positions.data_ptr(), pos_sb, A, split1, split2,
                                 inv_freq.data_ptr(), n_pairs, amplitude, 1 if layout == "interleaved" else 0, inverse,
-                                B, N, H, d, _stream_handle(stream))
+                                B, N, H, d, handle)
     if status:
         _check(status)
     return out
@@ -696,12 +704,12 @@ def kv4_append(cache, k_new, v_new, cache_len: int = 0, *, starts=None, stream=N
         raise ValueError("k_new must be 4-D [B, n_new, H, d]")
     n = k_new.shape[1]
     shape = (B, n, H, d)
-    ks = _check_view(k_new, "k_new", shape, (torch.bfloat16,))
-    vs = _check_view(v_new, "v_new", shape, (torch.bfloat16,))
+    ks = _check_view(k_new, "k_new", shape, torch.bfloat16)
+    vs = _check_view(v_new, "v_new", shape, torch.bfloat16)
     sp = _check_int32(starts, "starts", B)
-    _check_device(k_new, v_new, *cache, starts)
+    handle = _stream_on(k_new.get_device(), stream, v_new, *cache, starts)
     status = load().fastvr_kv4_append(*(t.data_ptr() for t in cache), k_new.data_ptr(), *ks, v_new.data_ptr(), *vs, sp,
-                                      B, H, d, cap, cache_len, n, _stream_handle(stream))
+                                      B, H, d, cap, cache_len, n, handle)
     if status:
         _check(status)
     return cache_len + n if starts is None else None
@@ -718,15 +726,15 @@ def kv4_read(cache, n: int, first: int = 0, *, starts=None, k_out=None, v_out=No
     if k_out is None:
         k_out = cache[0].new_empty(shape, dtype=torch.bfloat16)
     else:
-        ks = _check_view(k_out, "k_out", shape, (torch.bfloat16,))
+        ks = _check_view(k_out, "k_out", shape, torch.bfloat16)
     if v_out is None:
         v_out = _empty(k_out, shape, torch.bfloat16)
     else:
-        vs = _check_view(v_out, "v_out", shape, (torch.bfloat16,))
+        vs = _check_view(v_out, "v_out", shape, torch.bfloat16)
     sp = _check_int32(starts, "starts", B)
-    _check_device(k_out, v_out, *cache, starts)
+    handle = _stream_on(k_out.get_device(), stream, v_out, *cache, starts)
     status = load().fastvr_kv4_read(*(t.data_ptr() for t in cache), k_out.data_ptr(), *ks, v_out.data_ptr(), *vs, sp, B,
-                                    H, d, cap, first, n, _stream_handle(stream))
+                                    H, d, cap, first, n, handle)
     if status:
         _check(status)
     return k_out, v_out
@@ -758,20 +766,21 @@ def kv4_attn(q, cache, cache_len: int, *, lens=None, chunk_len: int | None = Non
     _, Nq, H, _ = shape
     if shape[0] != B or shape[3] != d:
         raise ValueError(f"shape mismatch: q {tuple(shape)}, cache of {B} sequences and head_dim {d}")
-    qs = _check_view(q, "q", shape, (bf16,))
+    qs = _check_view(q, "q", shape, bf16)
     if chunk_len is None:
         chunk_len = max(cache_len, 1)
     if scale is None:
         scale = 1.0 / math.sqrt(d)
     if out_dtype is None:
         out_dtype = out.dtype if out is not None else fp32
-    if out_dtype not in (bf16, fp32):
+    if out_dtype is not bf16 and out_dtype is not fp32:
         raise ValueError("out_dtype must be float32 or bfloat16")
+    handle = _stream_on(q.get_device(), stream, *cache, lens, out, lse, workspace)
     os_ = (Nq * H * d, H * d)
     if out is None:
         out = _empty(q, shape, out_dtype)
     else:
-        os_ = _check_view(out, "out", shape, (out_dtype,))
+        os_ = _check_view(out, "out", shape, out_dtype)
     if lse is not None:
         if lse.dtype != fp32 or lse.shape != (B, H, Nq) or not lse.is_contiguous():
             raise ValueError("lse must be a contiguous float32 [B, H, Nq] tensor")
@@ -786,11 +795,10 @@ def kv4_attn(q, cache, cache_len: int, *, lens=None, chunk_len: int | None = Non
         raise ValueError("workspace must be a contiguous uint8 tensor")
     else:
         n_ws = workspace.numel()
-    _check_device(q, *cache, lens, out, lse, workspace)
     status = load().fastvr_kv4_attn(q.data_ptr(), *qs, *(t.data_ptr() for t in cache), out.data_ptr(), *os_,
-                                    1 if out_dtype == bf16 else 0, lse.data_ptr() if lse is not None else None,
+                                    1 if out_dtype is bf16 else 0, lse.data_ptr() if lse is not None else None,
                                     workspace.data_ptr() if workspace is not None else None, n_ws, lp, B, H, Hkv, Nq, d,
-                                    cap, cache_len, chunk_len, window_chunks, scale, _stream_handle(stream))
+                                    cap, cache_len, chunk_len, window_chunks, scale, handle)
     if status:
         _check(status)
     return out, lse
