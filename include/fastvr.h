@@ -381,9 +381,9 @@ fastvr_status fastvr_kv4_read(const void* k_codes, const void* k_scales, const v
  * {64, 128}; H a multiple of Hkv; 0 <= cache_len <= capacity; chunk_len >= 1;
  * window_chunks >= -1; scale finite; cache tensors contiguous, 16-byte aligned; view
  * rules of fastvr_chunk_attn_fwd_ex for q and o; lens NULL or 4-byte aligned; o,
- * lse and workspace overlap nothing; capacity <= FASTVR_KV4_MAX_CAPACITY, Nq * H
- * and token strides below 2^31 and not more work items than one launch holds (else
- * FASTVR_ERR_UNSUPPORTED).
+ * lse and workspace overlap nothing; capacity <= FASTVR_KV4_MAX_CAPACITY, H <= 65535,
+ * Nq * H and token strides below 2^31 and not more work items than one launch holds
+ * (else FASTVR_ERR_UNSUPPORTED).
  * B, H or Nq equal to 0: FASTVR_OK, nothing enqueued.
  */
 fastvr_status fastvr_kv4_attn_workspace(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d, int64_t cache_len,

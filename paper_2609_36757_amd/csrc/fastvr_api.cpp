@@ -694,9 +694,9 @@ fastvr_status kv4_sizes(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d
     return FASTVR_OK;
   }
   int64_t rows;
-  if (B > INT32_MAX || H > INT32_MAX || Nq > INT32_MAX || !mul_ok(Nq, H, &rows) || rows > INT32_MAX ||
+  if (B > INT32_MAX || H > 65535 || Nq > INT32_MAX || !mul_ok(Nq, H, &rows) || rows > INT32_MAX ||
       !mul_ok(rows, B, &rows) || rows > (int64_t(1) << 36))
-    return fail(FASTVR_ERR_UNSUPPORTED, "sizes must be below 2^31, and B * H * Nq below 2^36");
+    return fail(FASTVR_ERR_UNSUPPORTED, "H > 65535, Nq * H not below 2^31, or B * H * Nq above 2^36");
   const fastvr::Kv4Plan plan = fastvr::kv4_plan(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks);
   if (plan.units > fastvr::kMaxKv4Units || (plan.n_split > 1 && rows > fastvr::kMaxKv4Units))
     return fail(FASTVR_ERR_UNSUPPORTED, "problem needs too many workgroups");

@@ -338,13 +338,14 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
       raise |= m[t] > bound[t];
     }
     if (__builtin_amdgcn_ballot_w64(raise)) {
-      // raise the reference of every row to its maximum so far (fmaxf drops NaN scores)
+      // raise the reference of the rows that need it to their maximum so far, those alone: a
+      // row's bits depend on the keys that it sees only (NaN scores raise nothing)
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
-        const float m_new = __builtin_fmaxf(mc[t], row_max4(m[t]) * p.c);
+        const float top = row_max4(m[t]), m_new = top > bound[t] ? top * p.c : mc[t];
         const float alpha = __builtin_amdgcn_exp2f(mc[t] - m_new);
         mc[t] = m_new;
-        bound[t] = (m_new + kSlack) * inv_c;
+        bound[t] = top > bound[t] ? (m_new + kSlack) * inv_c : bound[t];
         l[t] *= alpha;
 #pragma unroll
         for (int j = 0; j < kE; ++j) acc[t][j] *= alpha;

@@ -98,7 +98,7 @@ def test_cache_copies_empty(raw, kw):
     (dict(chunk_len=0), INV, "chunk_len"), (dict(window_chunks=-2), INV, "window_chunks"), (dict(capacity=8999), INV, "capacity"),
     (dict(capacity=1 << 25), UNS, "capacity"), (dict(cache_len=1 << 25, capacity=1 << 25), UNS, "cache_len"), (dict(scale=float("inf")), INV, "scale"),
     (dict(o_bf16=2), INV, "o_bf16"), (dict(q_st=500), INV, "token stride"), (dict(o_sb=512), INV, "batch stride"),
-    (dict(Nq=1 << 31), UNS, "2^31"), (dict(H=1 << 20, Hkv=1 << 20, Nq=1 << 12), UNS, "2^31"), (dict(B=1 << 30), UNS, ""),
+    (dict(Nq=1 << 31), UNS, "2^31"), (dict(H=65536, Hkv=65536), UNS, "65535"), (dict(H=32768, Hkv=32768, Nq=1 << 17), UNS, "2^31"), (dict(B=1 << 30), UNS, ""),
     (dict(o=Q), INV, "overlaps"), (dict(o=KC + 64), INV, "overlaps"), (dict(lse=O), INV, "overlaps"), (dict(workspace=VS), INV, "overlaps"),
     (dict(workspace=Q), INV, "overlaps"), (dict(lse=VC), INV, "overlaps"), (dict(lens=O + 8), INV, "overlaps"),
     (dict(q_st=1 << 31, q_sb=1 << 33), UNS, "strides"),

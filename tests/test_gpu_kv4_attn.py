@@ -196,3 +196,23 @@ def test_attn_refusals(dev):
     o, lse = fastvr.kv4_attn(q, cache, 0)
     assert (o == 0).all() and torch.isneginf(lse).all()
     assert fastvr.kv4_attn(q[:, :0], cache, n)[0].shape == (B, 0, H, d)
+
+
+def test_rows_do_not_depend_on_keys_they_do_not_see(dev):
+    """Token-causal rows that share tiles and steps: other keys behind a row, of any size, leave its
+    bits as they were."""
+    print("\n[gpu case] kv4 attn, keys behind a row", flush=True)
+    B, Nq, H, d, n = 1, 48, 2, 128, 500
+    q, cache, _, _ = inputs(B, Nq, H, H, d, n, n, 31)
+    o, lse = run(dev, q, cache, n, chunk_len=1)
+    other = [t.clone() for t in cache]
+    g = torch.Generator().manual_seed(32)
+    first = n - Nq // 2           # keys from here on change: larger, of both signs, one NaN
+    for i in (0, 2):
+        other[i][:, :, first:] = torch.randint(0, 256, other[i][:, :, first:].shape, generator=g, dtype=torch.uint8)
+        other[i + 1][:, :, first:] = 131
+    other[3][:, 0, n - 1, 1] = 255
+    o2, lse2 = run(dev, q, other, n, chunk_len=1)
+    same = first - (n - Nq)       # rows before the first changed key
+    assert torch.equal(o[:, :same], o2[:, :same]) and torch.equal(lse[..., :same], lse2[..., :same])
+    assert not torch.equal(o[:, same:], o2[:, same:])
