@@ -11,7 +11,6 @@
 #include <cstdio>
 #include <string>
 
-#include "kv4_plan.h"
 #include "launch.h"
 
 namespace {
@@ -673,9 +672,9 @@ fastvr_status kv4_copy(bool write, const void* kc, const void* ks, const void* v
   return ok();
 }
 
-// Sizes and mask of an attention over a 4-bit cache; *empty: nothing to do.
+// Sizes and mask of an attention over a 4-bit cache, and its plan; *empty: nothing to do.
 fastvr_status kv4_sizes(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d, int64_t cache_len,
-                        int64_t chunk_len, int64_t window_chunks, bool* empty) {
+                        int64_t chunk_len, int64_t window_chunks, bool* empty, fastvr::Kv4Plan* plan) {
   *empty = false;
   if (B < 0 || H < 0 || Hkv < 0 || Nq < 0 || cache_len < 0)
     return fail(FASTVR_ERR_INVALID_ARGUMENT, "negative size (B=%lld H=%lld Hkv=%lld Nq=%lld cache_len=%lld)",
@@ -697,8 +696,8 @@ fastvr_status kv4_sizes(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d
   if (B > INT32_MAX || H > 65535 || Nq > INT32_MAX || !mul_ok(Nq, H, &rows) || rows > INT32_MAX ||
       !mul_ok(rows, B, &rows) || rows > (int64_t(1) << 36))
     return fail(FASTVR_ERR_UNSUPPORTED, "H > 65535, Nq * H not below 2^31, or B * H * Nq above 2^36");
-  const fastvr::Kv4Plan plan = fastvr::kv4_plan(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks);
-  if (plan.units > fastvr::kMaxKv4Units || (plan.n_split > 1 && rows > fastvr::kMaxKv4Units))
+  *plan = fastvr::kv4_plan(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks);
+  if (plan->units > fastvr::kMaxKv4Units || (plan->n_split > 1 && rows > fastvr::kMaxKv4Units))
     return fail(FASTVR_ERR_UNSUPPORTED, "problem needs too many workgroups");
   return FASTVR_OK;
 }
@@ -790,9 +789,10 @@ fastvr_status fastvr_kv4_attn_workspace(int64_t B, int64_t H, int64_t Hkv, int64
                                         int64_t chunk_len, int64_t window_chunks, int64_t* bytes) {
   if (bytes == nullptr) return fail(FASTVR_ERR_INVALID_ARGUMENT, "bytes is NULL");
   bool empty;
-  const fastvr_status s = kv4_sizes(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks, &empty);
+  fastvr::Kv4Plan plan;
+  const fastvr_status s = kv4_sizes(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks, &empty, &plan);
   if (s != FASTVR_OK) return s;
-  *bytes = empty ? 0 : fastvr::kv4_plan(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks).ws_bytes;
+  *bytes = empty ? 0 : plan.ws_bytes;
   return ok();
 }
 
@@ -803,7 +803,8 @@ fastvr_status fastvr_kv4_attn(const void* q, int64_t q_sb, int64_t q_st, const v
                               int64_t capacity, int64_t cache_len, int64_t chunk_len, int64_t window_chunks,
                               float scale, void* stream) {
   bool empty;
-  fastvr_status s = kv4_sizes(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks, &empty);
+  fastvr::Kv4Plan plan;
+  fastvr_status s = kv4_sizes(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks, &empty, &plan);
   if (s != FASTVR_OK) return s;
   if (capacity < cache_len)
     return fail(FASTVR_ERR_INVALID_ARGUMENT, "cache_len = %lld > capacity = %lld", (long long)cache_len,
@@ -828,7 +829,6 @@ fastvr_status fastvr_kv4_attn(const void* q, int64_t q_sb, int64_t q_st, const v
     lb = B * H * Nq * 4;
   }
   if (!aligned(lens, 4)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "lens is not 4-byte aligned");
-  const fastvr::Kv4Plan plan = fastvr::kv4_plan(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks);
   if (plan.ws_bytes > 0) {
     if (workspace == nullptr || workspace_bytes < plan.ws_bytes)
       return fail(FASTVR_ERR_INVALID_ARGUMENT, "workspace of %lld bytes, %lld needed",
@@ -862,6 +862,7 @@ fastvr_status fastvr_kv4_attn(const void* q, int64_t q_sb, int64_t q_st, const v
   a.capacity = capacity; a.cache_len = cache_len;
   a.chunk_len = chunk_len; a.window_chunks = window_chunks;
   a.scale = scale;
+  a.plan = plan;
   if (fastvr::launch_kv4_attn == nullptr) return no_kernels("kv4_attn");
   const hipError_t e = fastvr::launch_kv4_attn(a, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(FASTVR_ERR_HIP, "kv4_attn launch failed: %s", hipGetErrorString(e));

@@ -585,7 +585,7 @@ hipError_t launch_t(const Kv4Params& p, const Kv4Plan& plan, hipStream_t stream)
 }  // namespace
 
 hipError_t launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t stream) {
-  const Kv4Plan plan = kv4_plan(a.B, a.H, a.Hkv, a.nq, a.d, a.cache_len, a.chunk_len, a.window_chunks);
+  const Kv4Plan& plan = a.plan;
   Kv4Params p;
   p.q = static_cast<const uint16_t*>(a.q);
   p.q_sb = a.q_sb;

@@ -45,8 +45,8 @@ constexpr int kv4_split_at(int n, int split, int n_split) { return (int)((int64_
 //    (head_dim 64: 0.85 of that), in as many rounds as do not fit at once (4, 2 and 2 on a CU);
 //  * the cache at 5.5 TB/s once, and from L2 at four times that for every other row tile; of
 //    this and the steps the shorter hides behind the longer by 70%;
-//  * from two workgroups a tile on the second kernel, 3 us and 3 us more on the host, 0.25 ns a
-//    row, and the partial results written and read.
+//  * from two workgroups a tile on the second kernel, 3 us and 3 us more on the host, 25 ns a
+//    workgroup, 0.25 ns a row, and the partial results written and read.
 // Measured, 12 heads, head_dim 128: one query over 65280 keys 318 us with 1 workgroup a tile, 87 with
 // 4, 27.9 with 16, 23.5 with 32; 64 queries over 1000 keys 9.3, 11.3 and 16.6 us with 1, 2 and 4 row
 // tiles, 3120 over 18720 keys 410 and 369 us with 2 and 4.
@@ -63,7 +63,7 @@ inline double kv4_time(int64_t tiles, int q, int64_t steps, double bytes, int64_
                                                 : (double)units / (double)kAtOnce[at] + 0.5;
   const double wait = step * (double)own * rounds, read = bytes / 5500.0;
   return kFixed[at] + (wait > read ? wait + 0.3 * read : read + 0.3 * wait) +
-         (s > 1 ? 6000.0 + 0.25 * (double)rows + (double)(rows * s * (d * 4 + 8) * 2) / 5000.0 : 0.0);
+         (s > 1 ? 6000.0 + 25.0 * (double)s + 0.25 * (double)rows + (double)(rows * s * (d * 4 + 8) * 2) / 5000.0 : 0.0);
 }
 
 // B, H, Hkv, nq >= 1; 0 <= cache_len; 1 <= chunk_len; window >= -1; H a multiple of Hkv.
@@ -85,17 +85,23 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
     }
     const int64_t steps = (keys + kKv4StepKeys - 1) / kKv4StepKeys + 1;
     const double bytes = (double)(B * Hkv * keys * (d / 2 + d / 32) * 2) * (1.0 + 0.25 * (double)(row_tiles - 1));
-    for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit}) {
+    constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit};
+    double times[sizeof(kSplits) / sizeof(int)], least = 0;
+    int n = 0;
+    for (int s : kSplits) {
       if (s > 1 && (s > steps || p.rows * s * (d * 4 + 8) > kKv4MaxWorkspace)) break;
-      const double time = kv4_time(tiles, q, steps, bytes, p.rows, d, s);
-      // (2%: no more partial results for nothing)
-      if (p.q_tiles == 0 || time < 0.98 * best) {
-        best = time;
-        p.q_tiles = q;
-        p.n_split = s;
-        p.row_tiles = row_tiles;
-      }
+      times[n] = kv4_time(tiles, q, steps, bytes, p.rows, d, s);
+      least = n == 0 || times[n] < least ? times[n] : least;
+      ++n;
     }
+    if (p.q_tiles != 0 && least >= best) continue;
+    best = least;
+    p.q_tiles = q;
+    p.row_tiles = row_tiles;
+    // of splits that take the same time the most: shorter sequences than the longest leave
+    // some of their workgroups nothing to do
+    while (times[n - 1] > 1.03 * least) --n;
+    p.n_split = kSplits[n - 1];
   }
   const int64_t tiles = B * Hkv * p.row_tiles;
   p.units = tiles * p.n_split;

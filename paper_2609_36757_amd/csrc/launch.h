@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "fastvr.h"
+#include "kv4_plan.h"
 
 namespace fastvr {
 
@@ -157,6 +158,7 @@ struct Kv4AttnArgs {
   const int32_t* lens;  // or null
   int64_t B, H, Hkv, nq, d, capacity, cache_len, chunk_len, window_chunks;
   float scale;
+  Kv4Plan plan;  // kv4_plan of these sizes
 };
 __attribute__((weak)) hipError_t launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t stream);
 

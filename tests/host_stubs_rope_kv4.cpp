@@ -4,7 +4,6 @@
 
 #include <cstdlib>
 
-#include "kv4_plan.h"
 #include "launch.h"
 
 namespace fastvr {
@@ -31,7 +30,8 @@ hipError_t launch_kv4_read(const Kv4CopyArgs& a, hipStream_t) { return holds(cop
 hipError_t launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t) {
   const Kv4Plan p = kv4_plan(a.B, a.H, a.Hkv, a.nq, a.d, a.cache_len, a.chunk_len, a.window_chunks);
   return holds(a.q && a.o && a.B > 0 && a.nq > 0 && a.H % a.Hkv == 0 && a.cache_len <= a.capacity && a.chunk_len >= 1 &&
-               p.units <= kMaxKv4Units && (p.ws_bytes == 0 || a.workspace) && (a.capacity == 0 || a.cache.k_codes));
+               p.units == a.plan.units && p.ws_bytes == a.plan.ws_bytes && p.units <= kMaxKv4Units &&
+               (p.ws_bytes == 0 || a.workspace) && (a.capacity == 0 || a.cache.k_codes));
 }
 
 }  // namespace fastvr
