@@ -215,6 +215,42 @@ def test_stream_argument(dev):
     compare(out, lse, kv4.attention(turned[:, :, :H], k, v, [n], chunk_len=n, scale=0.125), n, "stream argument")
 
 
+def test_stream_argument_allocates_there(dev):
+    """What a call on another stream allocates by itself, its workspace too, is that stream's memory: tensors
+    made and filled on the current stream while the call still waits for its turn take none of it."""
+    print("\n[gpu case] flow, allocations of another stream", flush=True)
+    s = torch.cuda.Stream()
+    B, H, d, n = 2, 12, 128, 4000
+    k, v = (projections(B, n, H, d, dev, seed)[:, :, :H] for seed in (8, 9))
+    q = projections(B, 1, H, d, dev, 10)[:, :, :H]
+    f = torch.tensor(fastvr.rope_inv_freq(64)[0], dtype=torch.float64, device=dev)
+    pos = torch.arange(n, dtype=torch.int32, device=dev)
+    cache = fastvr.kv4_cache(B, n, H, d, dev)
+    fastvr.kv4_append(cache, k, v)
+    n_ws = fastvr.kv4_attn_workspace(B, H, H, 1, d, n, n)
+    assert n_ws > 0
+    want = (*fastvr.kv4_attn(q, cache, n), fastvr.rope(k, pos, f), *fastvr.kv4_read(cache, n))
+    work = torch.randn((8192, 8192), device=dev)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        for _ in range(4):
+            work = work @ work                    # some 10 ms ahead of the calls
+    got = (*fastvr.kv4_attn(q, cache, n, stream=s), fastvr.rope(k, pos, f, stream=s),
+           *fastvr.kv4_read(cache, n, stream=s))
+    junk = [torch.full((max(1, size // 4),), float("nan"), device=dev)
+            for size in (n_ws, *(t.numel() * t.element_size() for t in got)) for _ in range(2)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert all(bool(t.isnan().all()) for t in junk)
+
+    class Elsewhere:
+        cuda_stream, device_index = 0, 1
+    for call in (lambda: fastvr.kv4_attn(q, cache, n, stream=Elsewhere), lambda: fastvr.rope(k, pos, f, stream=Elsewhere),
+                 lambda: fastvr.kv4_append(cache, k, v, stream=Elsewhere)):
+        with pytest.raises(ValueError, match="the stream is on cuda:1"):
+            call()
+
+
 def test_training_gradients(dev):
     """Loss gradients through rotary positions and the chunk attention: rope -> chunk_attn ->
     chunk_attn_bwd -> rope_bwd against the oracles' chain in fp64.  The attention's gradients differ from
