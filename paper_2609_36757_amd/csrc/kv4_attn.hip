@@ -5,11 +5,11 @@
 //
 // over the keys that row i sees, a contiguous interval [lo_i, hi_i).  The rows of one
 // key head are (token, head of the group) pairs in that order, so lo and hi do not
-// fall from row to row.  A workgroup takes a tile of 16 or 32 rows of one (batch,
-// key head) and a share of the keys that the tile sees; its four waves take steps of
-// 32 keys in turn, each with its own running maximum, sum and O, and join them
-// through LDS.  Where the tiles are few, the keys are split over several workgroups
-// and a second kernel joins their partial results (kv4_plan.h).
+// fall from row to row.  A workgroup takes 16, 32 or 64 rows (QT row tiles) of one
+// (batch, key head) and a share of the keys that they see; its four waves take steps
+// of 32 keys in turn, each with its own running maximum, sum and O, and join them
+// through LDS.  Where these workgroups are few, the keys are split over several of
+// them and a second kernel joins their partial results (kv4_plan.h).
 //
 // A step, one wave: S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_16x16x32_bf16.
 //  * K comes from the cache straight into registers: a lane holds a quarter of a key
@@ -24,8 +24,24 @@
 //  * The maximum a row is measured against is raised only when a score exceeds it by
 //    8 (in log2 units: P <= 2^8 then), so that most steps need no exchange between
 //    lanes and no rescale of O.
-// A step is about 200 vector instructions against 256 cycles of matrix core: for one
-// row tile, reading the cache from HBM takes longer than both.
+// What is rounded: P to bf16 for the products (half a step, 2^-8 of each weight; the
+// sums l and all of S, LSE and O are fp32), and O where bf16 is asked for.  K and V
+// are exact in bf16, so their products with Q and P are exact.  (The matrix
+// instruction that takes 4-bit operands and block scales itself would save K's
+// conversion, with Q in two 8-bit parts; its sums were off by 4e-5 of the largest, too
+// much for LSE.)
+//
+// What bounds it.  One row tile (a token of each sequence): the cache's bytes; a
+// step's 4.3 KB take longer than its 190 vector instructions and 256 cycles of matrix
+// core.  One query over 65280 keys of 12 heads: 20.7 us for 107 MB (5.1 TB/s, a copy's
+// rate), and 4 us for the join.  Four row tiles: conversion, exp2 and sums, 240 vector
+// instructions a step of 64 rows against 1024 cycles of matrix core; two waves of a
+// SIMD overlap them to 56% of the matrix core's time.  16320 queries over 65280 keys:
+// 5.1 ms, 1280 TFLOP/s (a large bf16 GEMM reaches 1500 on the same card, the bf16
+// forward on an expanded cache 1300).  What it took: Q in LDS and V's scales loaded
+// late, for two waves on a SIMD without a spilled register (15.9 ms with one wave on a
+// SIMD; 5.6 with two); products at a higher wave priority (5.4); V converted and
+// paired between the products (5.1).
 //
 // Keys a row does not see: their P is zero, and in the steps where that can happen
 // V blocks that are not finite (rows behind a sequence may hold anything) are taken

