@@ -4,15 +4,15 @@
 // the bf16 bits without sign: it orders infinities and NaN above all numbers); its
 // exponent E and the leading mantissa bits give the scale byte, E - 2, one more from
 // a mantissa of 1.75 on, at least 2 and at most 252 (so that all values are normal
-// bf16 numbers); the elements go through the converting instruction, which divides by the power of two and rounds to nearest even (its
-// results equal the format's rounding for every bf16 number, subnormal quotients and
-// saturation among them).
+// bf16 numbers); the elements go through the converting instruction, which divides by
+// the power of two and rounds to nearest even (its results equal the format's rounding
+// for every bf16 number, subnormal quotients and saturation among them).
 //
 // Both kernels are bound by HBM bandwidth: 2 bytes an element on the bf16 side, 0.53
-// on the cache's; 16320 tokens of 12 heads (127 MB) are appended in 23.6 us (5.4 TB/s)
-// and read back in 20.0 us (6.3 TB/s), one token of 16 sequences in 3.3 us, the
-// launch.  A lane takes 8 elements, 16 (8) lanes a token row of head_dim 128
-// (64), four lanes a block; lanes run over the tokens of one head, whose codes are
+// on the cache's; 16320 tokens of 12 heads (127 MB) are appended in 23.8 us (5.3 TB/s)
+// and read back in 20.0 us (6.3 TB/s), one token of 16 sequences in 3.3 and 2.4 us, a
+// launch.  A lane takes 8 elements, 16 (8) lanes a token row of head_dim 128 (64),
+// four lanes a block; lanes run over the tokens of one head, whose codes are
 // contiguous in the cache.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
