@@ -697,7 +697,7 @@ fastvr_status kv4_sizes(int64_t B, int64_t H, int64_t Hkv, int64_t Nq, int64_t d
       !mul_ok(rows, B, &rows) || rows > (int64_t(1) << 36))
     return fail(FASTVR_ERR_UNSUPPORTED, "H > 65535, Nq * H not below 2^31, or B * H * Nq above 2^36");
   *plan = fastvr::kv4_plan(B, H, Hkv, Nq, d, cache_len, chunk_len, window_chunks);
-  if (plan->units > fastvr::kMaxKv4Units || (plan->n_split > 1 && rows > fastvr::kMaxKv4Units))
+  if (plan->units > fastvr::kMaxKv4Units || plan->rows > fastvr::kMaxKv4Units)
     return fail(FASTVR_ERR_UNSUPPORTED, "problem needs too many workgroups");
   return FASTVR_OK;
 }

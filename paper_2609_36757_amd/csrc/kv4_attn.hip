@@ -77,11 +77,13 @@ struct Kv4Params {
   int32_t o_st;
   int32_t o_bf16;
   float* lse;
-  float* part;  // [row][split][D] unnormalised O, then [row][split] (maximum, sum)
+  // of the split tiles' rows: [row][split][D] unnormalised O, then [row][split] (maximum, sum)
+  float* part;
   const int32_t* lens;
   int32_t B, H, Hkv, G, nq, R, capacity, cache_len, chunk_len, window;
-  int32_t row_tiles, n_split, units;
-  int64_t rows;
+  int32_t row_tiles, whole, rest, n_split, units;  // rest: split tiles
+  int32_t tile_rows;                               // rows with partial results in each of them
+  int64_t rows;                                    // in all of them
   float c;  // |scale| * log2(e)
   uint32_t sign;  // flips q for a negative scale
 };
@@ -139,11 +141,21 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
-  // workgroup -> (batch, key head), split, row tile; row tiles of one key range run
-  // next to each other on one XCD and share its L2
-  const int u = p.row_tiles > 1 ? xcd_unit(blockIdx.x, p.units) : (int)blockIdx.x;
-  const int tile = u % p.row_tiles, us = u / p.row_tiles;
-  const int split = us % p.n_split, bh = us / p.n_split;
+  // workgroup -> tile of all (batch, key head)s' row tiles, and split: first the whole tiles,
+  // then the others, row_tiles of them at a time with all their splits.  Row tiles of one key range
+  // run next to each other on one XCD and share its L2.
+  const bool alone = (int)blockIdx.x < p.whole;
+  const int blk = alone ? (int)blockIdx.x : (int)blockIdx.x - p.whole;
+  int at = p.row_tiles > 1 ? xcd_unit(blk, alone ? p.whole : p.units - p.whole) : blk, split = 0;
+  if (!alone) {
+    const int group = at / (p.row_tiles * p.n_split), first = group * p.row_tiles;
+    const int n_here = p.rest - first < p.row_tiles ? p.rest - first : p.row_tiles;
+    const int in = at - first * p.n_split;
+    split = in / n_here;
+    at = p.whole + first + in - split * n_here;
+  }
+  const int n_split = alone ? 1 : p.n_split;
+  const int bh = at / p.row_tiles, tile = at - bh * p.row_tiles;
   const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
   int len = p.cache_len;
   if (p.lens != nullptr) {
@@ -249,7 +261,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   // steps of this workgroup, [begin, end); in steps [in_lo, in_hi) all rows see all keys
   const int s0 = lo_min / kKv4StepKeys;
   const int n_steps = hi_max > lo_min ? (hi_max + kKv4StepKeys - 1) / kKv4StepKeys - s0 : 0;
-  const int begin = s0 + kv4_split_at(n_steps, split, p.n_split), end = s0 + kv4_split_at(n_steps, split + 1, p.n_split);
+  const int begin = s0 + kv4_split_at(n_steps, split, n_split), end = s0 + kv4_split_at(n_steps, split + 1, n_split);
   const int in_lo = (lo_max + kKv4StepKeys - 1) / kKv4StepKeys, in_hi = hi_min / kKv4StepKeys;
   int st = begin + wave;
   if (st < end) {
@@ -486,18 +498,18 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
 #pragma unroll
         for (int w = 0; w < kKv4Waves; ++w) v[j] += sm_o[(w * 16 + rr) * kPitch + e0 + j];
       }
-      const int i = r / p.G, h = hk * p.G + r - i * p.G;
-      const int64_t out_row = ((int64_t)b * p.H + h) * p.nq + i;
-      if (p.n_split > 1) {
-        float* dst = p.part + (out_row * p.n_split + split) * D + e0;
+      if (!alone) {
+        const int64_t row = (int64_t)(at - p.whole) * p.tile_rows + t * 16 + rr;
+        float* dst = p.part + (row * p.n_split + split) * D + e0;
 #pragma unroll
         for (int j = 0; j < kE; j += 4) *reinterpret_cast<f32x4*>(dst + j) = f32x4{v[j], v[j + 1], v[j + 2], v[j + 3]};
         if (e0 == 0) {
-          float* ml = p.part + p.rows * p.n_split * D + (out_row * p.n_split + split) * 2;
+          float* ml = p.part + p.rows * p.n_split * D + (row * p.n_split + split) * 2;
           ml[0] = m;
           ml[1] = sum;
         }
       } else {
+        const int i = r / p.G, h = hk * p.G + r - i * p.G;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const int64_t e = (int64_t)b * p.o_sb + (int64_t)i * p.o_st + h * D + e0;
         if (p.o_bf16) {
@@ -512,7 +524,8 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
           for (int j = 0; j < kE; j += 4)
             *reinterpret_cast<f32x4*>(dst + j) = f32x4{v[j] * inv, v[j + 1] * inv, v[j + 2] * inv, v[j + 3] * inv};
         }
-        if (e0 == 0 && p.lse != nullptr) p.lse[out_row] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
+        if (e0 == 0 && p.lse != nullptr)
+          p.lse[((int64_t)b * p.H + h) * p.nq + i] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
       }
     }
   }
@@ -527,7 +540,10 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
   __shared__ float sm[WAVES == 1 ? 1 : kKv4Waves][D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * kKv4Waves + wave : (int64_t)blockIdx.x;
-  if (row >= p.rows) return;  // (whole waves, and with WAVES = 4 whole workgroups)
+  const int j = (int)(row / p.tile_rows), bh = (p.whole + j) / p.row_tiles;
+  const int r = (p.whole + j - bh * p.row_tiles) * p.tile_rows + (int)(row - (int64_t)j * p.tile_rows);
+  // (whole waves, and with WAVES = 4 whole workgroups; the last tile of a head may have fewer rows)
+  if (row >= p.rows || r >= p.R) return;
   const int first = WAVES == 1 ? 0 : wave;
   const float* src = p.part + row * p.n_split * D + lane * kE;
   float x[kMine][kE];
@@ -563,9 +579,8 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
       v[j] = (sm[0][lane * kE + j] + sm[1 % WAVES][lane * kE + j]) + (sm[2 % WAVES][lane * kE + j] + sm[3 % WAVES][lane * kE + j]);
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const int i = (int)(row % p.nq);
-  const int64_t bh = row / p.nq;
-  const int64_t e = bh / p.H * p.o_sb + (int64_t)i * p.o_st + (int)(bh % p.H) * D + lane * kE;
+  const int b = bh / p.Hkv, i = r / p.G, h = (bh - b * p.Hkv) * p.G + r - i * p.G;
+  const int64_t e = (int64_t)b * p.o_sb + (int64_t)i * p.o_st + h * D + lane * kE;
 #pragma unroll
   for (int j = 0; j < kE; ++j) {
     if (p.o_bf16)
@@ -573,7 +588,8 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
     else
       static_cast<float*>(p.o)[e + j] = v[j] * inv;
   }
-  if (lane == 0 && p.lse != nullptr) p.lse[row] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
+  if (lane == 0 && p.lse != nullptr)
+    p.lse[((int64_t)b * p.H + h) * p.nq + i] = sum == 0.f ? -kInf : (m + __builtin_log2f(sum)) * kLn2;
 }
 
 template <int D>
@@ -631,7 +647,10 @@ hipError_t launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t stream) {
   p.chunk_len = (int32_t)L;
   p.window = (int32_t)(a.window_chunks > a.cache_len / L ? -1 : a.window_chunks);
   p.row_tiles = (int32_t)plan.row_tiles;
+  p.whole = (int32_t)plan.whole;
+  p.rest = (int32_t)(a.B * a.Hkv * plan.row_tiles - plan.whole);
   p.n_split = plan.n_split;
+  p.tile_rows = plan.row_tiles > 1 ? 16 * plan.q_tiles : p.R;
   p.units = (int32_t)plan.units;
   p.rows = plan.rows;
   // (not 0: masked scores, -inf * c, stay -inf; 2^-126 leaves P at 1 for all others)

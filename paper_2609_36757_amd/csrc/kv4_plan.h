@@ -1,5 +1,5 @@
 // Work plan of the attention over a 4-bit cache (host code, plain C++, no HIP
-// calls): tile height, and over how many workgroups the keys of a tile are split.
+// calls): tile height, which tiles' keys are split, and over how many workgroups.
 // It depends on the call's sizes only, so that the workspace can be asked for
 // beforehand; lengths on the device only shorten what a workgroup does.
 #pragma once
@@ -13,9 +13,10 @@ namespace fastvr {
 struct Kv4Plan {
   int32_t q_tiles;    // 16-row tiles of a workgroup: 1, 2 or 4
   int64_t row_tiles;  // workgroups over the rows of one (batch, key head)
-  int32_t n_split;    // workgroups over the keys of one tile
+  int64_t whole;      // tiles, the first ones, whose keys one workgroup walks
+  int32_t n_split;    // workgroups over the keys of each of the others
   int64_t units;      // workgroups
-  int64_t rows;       // rows of the call: B * H * Nq
+  int64_t rows;       // rows with partial results: those of the split tiles
   int64_t ws_bytes;
 };
 
@@ -49,19 +50,25 @@ constexpr int kv4_split_at(int n, int split, int n_split) { return (int)((int64_
 //    workgroup, 0.25 ns a row, and the partial results written and read.
 // Measured, 12 heads, head_dim 128: one query over 65280 keys 318 us with 1 workgroup a tile, 87 with
 // 4, 27.9 with 16, 23.5 with 32; 64 queries over 1000 keys 9.3, 11.3 and 16.6 us with 1, 2 and 4 row
-// tiles, 3120 over 18720 keys 410 and 369 us with 2 and 4.
-inline double kv4_time(int64_t tiles, int q, int64_t steps, double bytes, int64_t rows, int64_t d, int64_t s) {
+// tiles, 3120 over 18720 keys 410 and 369 us with 2 and 4 (all tiles split), 323 with 4 and 512 of the 588
+// tiles whole; 6000 over 65280 keys 2286 us with all tiles whole, 1989 with 1024 of 1128.
+// With `whole` tiles ahead that are not split, these take as long as whole rounds, filled or not, since
+// the others' workgroups take the places that are left; each workgroup of the others then adds half of
+// what it needs besides its steps.
+inline double kv4_time(int64_t whole, int64_t tiles, int q, int64_t steps, double bytes, int64_t rows, int64_t d,
+                       int64_t s) {
   const int at = q == 1 ? 0 : (q == 2 ? 1 : 2);
   constexpr double kFixed[3] = {4300, 5500, 8000}, kWait[3] = {630, 650, 1080}, kBusy[3] = {400, 600, 830};
   constexpr int64_t kAtOnce[3] = {4 * 256, 2 * 256, 2 * 256};
-  const int64_t units = tiles * s, here = units < kAtOnce[at] ? units : kAtOnce[at];
+  const int64_t units = tiles * s, all = whole + units, here = all < kAtOnce[at] ? all : kAtOnce[at];
   const int64_t own = ((steps + s - 1) / s + kKv4Waves - 1) / kKv4Waves;
   const double busy = kBusy[at] * (double)((here + 255) / 256);
   const double step = (kWait[at] > busy ? kWait[at] : busy) * (d == 128 ? 1.0 : 0.85);
   // (many rounds overlap, only their last one is not full)
   const double rounds = units < 4 * kAtOnce[at] ? (double)((units + kAtOnce[at] - 1) / kAtOnce[at])
                                                 : (double)units / (double)kAtOnce[at] + 0.5;
-  const double wait = step * (double)own * rounds, read = bytes / 5500.0;
+  const double ahead = (double)whole / (double)kAtOnce[at] * step * (double)((steps + kKv4Waves - 1) / kKv4Waves);
+  const double wait = (step * (double)own + (whole > 0 ? 0.5 * kFixed[at] : 0.0)) * rounds + ahead, read = bytes / 5500.0;
   return kFixed[at] + (wait > read ? wait + 0.3 * read : read + 0.3 * wait) +
          (s > 1 ? 6000.0 + 25.0 * (double)s + 0.25 * (double)rows + (double)(rows * s * (d * 4 + 8) * 2) / 5000.0 : 0.0);
 }
@@ -71,7 +78,7 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
                         int64_t window) {
   Kv4Plan p{};
   const int64_t G = H / Hkv, R = nq * G;
-  p.rows = B * H * nq;
+  constexpr int64_t kAtOnce[5] = {0, 4 * 256, 2 * 256, 0, 2 * 256};
   double best = 0;
   for (int q : {4, 2, 1}) {
     if (q > 1 && R <= 8 * q) continue;  // half of the rows, and more, would be empty
@@ -85,28 +92,34 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
     }
     const int64_t steps = (keys + kKv4StepKeys - 1) / kKv4StepKeys + 1;
     const double bytes = (double)(B * Hkv * keys * (d / 2 + d / 32) * 2) * (1.0 + 0.25 * (double)(row_tiles - 1));
-    constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit};
-    double times[sizeof(kSplits) / sizeof(int)], least = 0;
-    int n = 0;
-    for (int s : kSplits) {
-      if (s > 1 && (s > steps || p.rows * s * (d * 4 + 8) > kKv4MaxWorkspace)) break;
-      times[n] = kv4_time(tiles, q, steps, bytes, p.rows, d, s);
-      least = n == 0 || times[n] < least ? times[n] : least;
-      ++n;
+    // all tiles split alike, or only those that would fill a last round in part
+    const int64_t full = tiles / kAtOnce[q] * kAtOnce[q];
+    for (int tail = 0; tail < (full > 0 && full < tiles ? 2 : 1); ++tail) {
+      const int64_t whole = tail ? full : 0, rest = tiles - whole, rows = rest * (row_tiles > 1 ? tile : R);
+      constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit};
+      double times[sizeof(kSplits) / sizeof(int)], least = 0;
+      int n = 0;
+      for (int s : kSplits) {
+        if (s > 1 && (s > steps || rows * s * (d * 4 + 8) > kKv4MaxWorkspace)) break;
+        times[n] = kv4_time(whole, rest, q, steps, bytes, rows, d, s);
+        least = n == 0 || times[n] < least ? times[n] : least;
+        ++n;
+      }
+      if (p.q_tiles != 0 && least >= best) continue;
+      best = least;
+      p.q_tiles = q;
+      p.row_tiles = row_tiles;
+      // of splits that take the same time the most: shorter sequences than the longest leave
+      // some of their workgroups nothing to do
+      while (times[n - 1] > (tail ? 1.0 : 1.03) * least) --n;
+      p.n_split = kSplits[n - 1];
+      p.whole = p.n_split > 1 ? whole : tiles;
+      p.rows = p.n_split > 1 ? rows : 0;
     }
-    if (p.q_tiles != 0 && least >= best) continue;
-    best = least;
-    p.q_tiles = q;
-    p.row_tiles = row_tiles;
-    // of splits that take the same time the most: shorter sequences than the longest leave
-    // some of their workgroups nothing to do
-    while (times[n - 1] > 1.03 * least) --n;
-    p.n_split = kSplits[n - 1];
   }
-  const int64_t tiles = B * Hkv * p.row_tiles;
-  p.units = tiles * p.n_split;
+  p.units = p.whole + (B * Hkv * p.row_tiles - p.whole) * p.n_split;
   // partial results of each (row, split): O, then maximum and sum
-  p.ws_bytes = p.n_split > 1 ? p.rows * p.n_split * (d * 4 + 8) : 0;
+  p.ws_bytes = p.rows * p.n_split * (d * 4 + 8);
   return p;
 }
 

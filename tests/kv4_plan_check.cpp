@@ -51,6 +51,7 @@ int main() {
     CHECK(lo == n - 1 && hi == n);
   }
   // plans: every step of every tile belongs to one workgroup, sizes and workspace agree
+  long with_whole = 0;
   std::mt19937 rng(7);
   auto pick = [&](int64_t lo, int64_t hi) { return std::uniform_int_distribution<int64_t>(lo, hi)(rng); };
   auto log_pick = [&](double hi) { return (int64_t)std::exp2(std::uniform_real_distribution<double>(0, hi)(rng)); };
@@ -60,11 +61,15 @@ int main() {
     const Kv4Plan p = kv4_plan(B, Hkv * G, Hkv, nq, d, n, L, W);
     CHECK(p.q_tiles == 1 || p.q_tiles == 2 || p.q_tiles == 4);
     CHECK(p.row_tiles * 16 * p.q_tiles >= nq * G && (p.row_tiles - 1) * 16 * p.q_tiles < nq * G);
-    CHECK(p.n_split >= 1 && p.n_split <= kKv4MaxSplit && p.units == B * Hkv * p.row_tiles * p.n_split);
-    CHECK(p.rows == B * Hkv * G * nq);
-    CHECK(p.ws_bytes == (p.n_split > 1 ? p.rows * p.n_split * (d * 4 + 8) : 0) && p.ws_bytes <= kKv4MaxWorkspace);
+    CHECK(p.n_split >= 1 && p.n_split <= kKv4MaxSplit && p.whole >= 0);
+    const int64_t tiles = B * Hkv * p.row_tiles, rest = tiles - p.whole;
+    CHECK(p.n_split > 1 ? rest > 0 : rest == 0);
+    CHECK(p.units == p.whole + rest * p.n_split);
+    CHECK(p.rows == rest * (p.row_tiles > 1 ? 16 * p.q_tiles : nq * G));
+    CHECK(p.ws_bytes == p.rows * p.n_split * (d * 4 + 8) && p.ws_bytes <= kKv4MaxWorkspace);
+    with_whole += p.n_split > 1 && p.whole > 0;
     const Kv4Plan again = kv4_plan(B, Hkv * G, Hkv, nq, d, n, L, W);
-    CHECK(again.n_split == p.n_split && again.ws_bytes == p.ws_bytes);
+    CHECK(again.n_split == p.n_split && again.whole == p.whole && again.ws_bytes == p.ws_bytes);
     const int steps = (int)(n / kKv4StepKeys + 1);
     int at = 0;
     for (int s = 0; s < p.n_split; ++s) {
@@ -74,6 +79,7 @@ int main() {
     CHECK(at == steps);
     ++cases;
   }
+  CHECK(with_whole > 100);
   std::printf("%ld cases ok\n", cases);
   return 0;
 }

@@ -74,6 +74,37 @@ def test_attn_parity(dev, case):
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("case", [
+    # B, Nq, H, Hkv, d, n, chunk_len, window, output type
+    (33, 1, 33, 33, 64, 1500, None, -1, FP32),
+    (1, 2100, 8, 2, 128, 5003, None, -1, BF16),
+    (1, 4300, 8, 1, 64, 4300, 700, 2, FP32),
+    (2, 2200, 8, 1, 128, 2600, 1, -1, FP32),
+], ids=lambda c: f"B{c[0]}q{c[1]}H{c[2]}of{c[3]}d{c[4]}n{c[5]}L{c[6]}W{c[7]}")
+def test_more_tiles_than_fit_at_once(dev, case):
+    """One workgroup for the keys of most row tiles, several for those of the last ones: full
+    lengths, and lengths that leave some workgroups without keys.  Where key heads are many, three are made
+    and repeated; the oracle takes the first and the last sequence and one query head of each of their key heads."""
+    B, Nq, H, Hkv, d, n, L, W, ot = case
+    print(f"\n[gpu case] kv4 attn, many tiles {case}", flush=True)
+    ws = fastvr.kv4_attn_workspace(B, H, Hkv, Nq, d, n, L or n, W)
+    assert 0 < ws < B * H * Nq * (4 * d + 8)          # fewer than the rows have partial results
+    made = min(Hkv, 3)
+    _, cache, k, v = inputs(1, 1, made, made, d, n, n + 3, n + Nq)
+    cache = fastvr.KV4Cache(*(t.repeat(B, Hkv // made, 1, 1) for t in cache))
+    q = torch.randn((B, Nq, H, d), generator=torch.Generator().manual_seed(Nq)).to(BF16)
+    scale = float(np.float32(1 / math.sqrt(d)))
+    heads = [hk * (H // Hkv) + hk * 5 % (H // Hkv) for hk in list(range(Hkv))[-made:]]
+    for lens in ([n] * B, [n - (b * 37 + 900) % n for b in range(B)]):
+        t = torch.tensor(lens, dtype=torch.int32, device=dev)
+        o, lse = run(dev, q, cache, n, lens=t, chunk_len=L, window_chunks=W, out_dtype=ot)
+        for b in sorted({0, B - 1}):
+            ref = kv4.attention(q[b:b + 1, :, heads], k, v, lens[b:b + 1], chunk_len=L or n, window_chunks=W, scale=scale)
+            compare(o[b:b + 1, :, heads], lse[b:b + 1, heads], ref, n, f"{case} {b} {lens[b]}")
+        o2, lse2 = run(dev, q, cache, n, lens=t, chunk_len=L, window_chunks=W, out_dtype=ot)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
 @pytest.mark.parametrize("Nq,L,W", [(1, None, -1), (1, 1, 99), (6, 1, -1), (40, 16, 1)])
 def test_lengths_on_the_device(dev, Nq, L, W):
     """Lengths from none to all, fewer than Nq, and outside 0 .. cache_len; rows that see nothing."""
