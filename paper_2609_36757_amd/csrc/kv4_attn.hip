@@ -81,7 +81,7 @@ struct Kv4Params {
   float* part;
   const int32_t* lens;
   int32_t B, H, Hkv, G, nq, R, capacity, cache_len, chunk_len, window;
-  int32_t row_tiles, whole, rest, n_split, units;  // rest: split tiles
+  int32_t row_tiles, runs, whole, rest, n_split, units;  // rest: split tiles
   int32_t tile_rows;                               // rows with partial results in each of them
   int64_t rows;                                    // in all of them
   float c;  // |scale| * log2(e)
@@ -146,17 +146,17 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   // run next to each other on one XCD and share its L2.
   const bool alone = (int)blockIdx.x < p.whole;
   const int blk = alone ? (int)blockIdx.x : (int)blockIdx.x - p.whole;
-  int at = p.row_tiles > 1 ? xcd_unit(blk, alone ? p.whole : p.units - p.whole) : blk, split = 0;
+  int at = p.runs > 0 ? xcd_unit(blk, alone ? p.whole : p.units - p.whole) : blk, split = 0;
   if (!alone) {
-    const int group = at / (p.row_tiles * p.n_split), first = group * p.row_tiles;
+    const int group = (int)((uint32_t)at / (uint32_t)(p.row_tiles * p.n_split)), first = group * p.row_tiles;
     const int n_here = p.rest - first < p.row_tiles ? p.rest - first : p.row_tiles;
     const int in = at - first * p.n_split;
-    split = in / n_here;
+    split = (int)((uint32_t)in / (uint32_t)n_here);
     at = p.whole + first + in - split * n_here;
   }
   const int n_split = alone ? 1 : p.n_split;
-  const int bh = at / p.row_tiles, tile = at - bh * p.row_tiles;
-  const int b = bh / p.Hkv, hk = bh - b * p.Hkv;
+  const int bh = (int)((uint32_t)at / (uint32_t)p.row_tiles), tile = kv4_tile(at - bh * p.row_tiles, p.row_tiles, p.runs);
+  const int b = (int)((uint32_t)bh / (uint32_t)p.Hkv), hk = bh - b * p.Hkv;
   int len = p.cache_len;
   if (p.lens != nullptr) {
     const int l = p.lens[b];
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   const int row0 = tile * kRows;
   const int row_last = (row0 + kRows < p.R ? row0 + kRows : p.R) - 1;
   int lo_min, hi_min, lo_max, hi_max;
-  kv4_interval(len - p.nq + row0 / p.G, len, p.chunk_len, p.window, &lo_min, &hi_min);
-  kv4_interval(len - p.nq + row_last / p.G, len, p.chunk_len, p.window, &lo_max, &hi_max);
+  kv4_interval(len - p.nq + (int)((uint32_t)row0 / (uint32_t)p.G), len, p.chunk_len, p.window, &lo_min, &hi_min);
+  kv4_interval(len - p.nq + (int)((uint32_t)row_last / (uint32_t)p.G), len, p.chunk_len, p.window, &lo_max, &hi_max);
 
   f32x4 acc[QT][kE];
   // reference in log2 units, the score from which it is raised, sum of this lane's keys
@@ -261,9 +261,10 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   // steps of this workgroup, [begin, end); in steps [in_lo, in_hi) all rows see all keys
   const int s0 = lo_min / kKv4StepKeys;
   const int n_steps = hi_max > lo_min ? (hi_max + kKv4StepKeys - 1) / kKv4StepKeys - s0 : 0;
-  const int begin = s0 + kv4_split_at(n_steps, split, n_split), end = s0 + kv4_split_at(n_steps, split + 1, n_split);
+  const int begin = s0 + kv4_split_at(n_steps, split, n_split);
+  const int end = __builtin_amdgcn_readfirstlane(s0 + kv4_split_at(n_steps, split + 1, n_split));
   const int in_lo = (lo_max + kKv4StepKeys - 1) / kKv4StepKeys, in_hi = hi_min / kKv4StepKeys;
-  int st = begin + wave;
+  int st = __builtin_amdgcn_readfirstlane(begin + wave);
   if (st < end) {
     load_k(st);
     load_v(st);
@@ -272,7 +273,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   u32x4 q[kQLds ? 1 : QT][kKK];
   auto load_q = [&](int t, u32x4(&dst)[kKK]) {
     const int rt = row0 + t * 16 + n, r = rt <= row_last ? rt : row_last;
-    const int i = r / p.G, h = hk * p.G + r - i * p.G;
+    const int i = (int)((uint32_t)r / (uint32_t)p.G), h = hk * p.G + r - i * p.G;
     const uint16_t* src = p.q + (int64_t)b * p.q_sb + (int64_t)i * p.q_st + h * D + g * (D / 4);
 #pragma unroll
     for (int kk = 0; kk < kKK; ++kk) dst[kk] = *reinterpret_cast<const u32x4*>(src + kk * 8) ^ p.sign;
@@ -290,7 +291,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   if (tid < kRows) {
     const int r = row0 + tid <= row_last ? row0 + tid : row_last;
     int lo, hi;
-    kv4_interval(len - p.nq + r / p.G, len, p.chunk_len, p.window, &lo, &hi);
+    kv4_interval(len - p.nq + (int)((uint32_t)r / (uint32_t)p.G), len, p.chunk_len, p.window, &lo, &hi);
     sm_lo[tid] = lo;
     sm_n[tid] = hi - lo;
   }
@@ -509,7 +510,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
           ml[1] = sum;
         }
       } else {
-        const int i = r / p.G, h = hk * p.G + r - i * p.G;
+        const int i = (int)((uint32_t)r / (uint32_t)p.G), h = hk * p.G + r - i * p.G;
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const int64_t e = (int64_t)b * p.o_sb + (int64_t)i * p.o_st + h * D + e0;
         if (p.o_bf16) {
@@ -539,9 +540,11 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
   static_assert(kMine * kKv4Waves == kKv4MaxSplit, "every split has a wave");
   __shared__ float sm[WAVES == 1 ? 1 : kKv4Waves][D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * kKv4Waves + wave : (int64_t)blockIdx.x;
-  const int j = (int)(row / p.tile_rows), bh = (p.whole + j) / p.row_tiles;
-  const int r = (p.whole + j - bh * p.row_tiles) * p.tile_rows + (int)(row - (int64_t)j * p.tile_rows);
+  // (32 bits: a launch has fewer than 2^24 workgroups)
+  const uint32_t row32 = WAVES == 1 ? blockIdx.x * kKv4Waves + wave : blockIdx.x, row_tiles = p.row_tiles;
+  const uint32_t j = row32 / (uint32_t)p.tile_rows, at = p.whole + j, bh = at / row_tiles;
+  const int r = kv4_tile((int)(at - bh * row_tiles), p.row_tiles, p.runs) * p.tile_rows + (int)(row32 - j * p.tile_rows);
+  const int64_t row = row32;
   // (whole waves, and with WAVES = 4 whole workgroups; the last tile of a head may have fewer rows)
   if (row >= p.rows || r >= p.R) return;
   const int first = WAVES == 1 ? 0 : wave;
@@ -579,7 +582,8 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
       v[j] = (sm[0][lane * kE + j] + sm[1 % WAVES][lane * kE + j]) + (sm[2 % WAVES][lane * kE + j] + sm[3 % WAVES][lane * kE + j]);
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const int b = bh / p.Hkv, i = r / p.G, h = (bh - b * p.Hkv) * p.G + r - i * p.G;
+  const int b = (int)(bh / (uint32_t)p.Hkv), i = (int)((uint32_t)r / (uint32_t)p.G);
+  const int h = ((int)bh - b * p.Hkv) * p.G + r - i * p.G;
   const int64_t e = (int64_t)b * p.o_sb + (int64_t)i * p.o_st + h * D + lane * kE;
 #pragma unroll
   for (int j = 0; j < kE; ++j) {
@@ -647,6 +651,7 @@ hipError_t launch_kv4_attn(const Kv4AttnArgs& a, hipStream_t stream) {
   p.chunk_len = (int32_t)L;
   p.window = (int32_t)(a.window_chunks > a.cache_len / L ? -1 : a.window_chunks);
   p.row_tiles = (int32_t)plan.row_tiles;
+  p.runs = kv4_runs(p.row_tiles);
   p.whole = (int32_t)plan.whole;
   p.rest = (int32_t)(a.B * a.Hkv * plan.row_tiles - plan.whole);
   p.n_split = plan.n_split;

@@ -30,13 +30,30 @@ constexpr int64_t kKv4MaxWorkspace = int64_t(64) << 20;
 constexpr void kv4_interval(int pos, int len, int chunk_len, int window, int* lo, int* hi) {
   *lo = *hi = 0;
   if (pos < 0) return;
-  const int c = pos / chunk_len, first = c * chunk_len;
+  const int c = (int)((uint32_t)pos / (uint32_t)chunk_len), first = c * chunk_len;
   if (window >= 0 && c > window) *lo = first - window * chunk_len;
   *hi = len - first > chunk_len ? first + chunk_len : len;
 }
 
+// Order of a head's row tiles.  Later rows may see more keys, so they go first.  The units of a
+// round of 256 are dealt to the 8 XCDs in runs of 32 (xcd_unit) that share an L2; so that every run has
+// tiles from all over the head, run j of `runs` holds the tiles j, j + runs, ... from the end.  With 256 tiles
+// and more a round is one head's, dealing its units one by one does the same (0 runs).  32 query heads on 8, 8192
+// queries over 8192 keys that see the ones before them: 690 us in rising order, an XCD having the longest 32
+// tiles of each round, 510 in this one.
+constexpr int kv4_runs(int row_tiles) { return row_tiles >= 256 || row_tiles <= 1 ? 0 : (row_tiles + 31) / 32; }
+constexpr int kv4_tile(int i, int row_tiles, int runs) {
+  if (runs <= 1) return row_tiles - 1 - i;
+  const int len = (int)((uint32_t)row_tiles / (uint32_t)runs), longer = row_tiles - len * runs;
+  const int split = longer * (len + 1);  // the first `longer` runs hold one tile more
+  const int of = i < split ? len + 1 : len, from = i < split ? i : i - split;
+  const int run = (int)((uint32_t)from / (uint32_t)of), in = from - run * of;
+  return row_tiles - 1 - (in * runs + run + (i < split ? 0 : longer));
+}
+
 // First of n steps that workgroup `split` of `n_split` takes (the next one's first ends them).
-constexpr int kv4_split_at(int n, int split, int n_split) { return (int)((int64_t)n * split / n_split); }
+// (n * split <= 2^19 * 64; a division of 64 bits would take longer than a step's loads)
+constexpr int kv4_split_at(int n, int split, int n_split) { return (int)((uint32_t)n * (uint32_t)split / (uint32_t)n_split); }
 
 // Time of a call in ns with q row tiles a workgroup (of `tiles` such tiles) and s
 // workgroups over the keys of each, from measurements on a chip with 256 CUs:
@@ -51,12 +68,15 @@ constexpr int kv4_split_at(int n, int split, int n_split) { return (int)((int64_
 // Measured, 12 heads, head_dim 128: one query over 65280 keys 318 us with 1 workgroup a tile, 87 with
 // 4, 27.9 with 16, 23.5 with 32; 64 queries over 1000 keys 9.3, 11.3 and 16.6 us with 1, 2 and 4 row
 // tiles, 3120 over 18720 keys 410 and 369 us with 2 and 4 (all tiles split), 323 with 4 and 512 of the 588
-// tiles whole; 6000 over 65280 keys 2286 us with all tiles whole, 1989 with 1024 of 1128.
+// tiles whole; 6000 over 65280 keys 2286 us with all tiles whole, 1989 with 1024 of 1128.  4000 queries over 4000
+// keys that see the ones before them: 79 us as if all tiles took the longest one's time, 76 now.
 // With `whole` tiles ahead that are not split, these take as long as whole rounds, filled or not, since
 // the others' workgroups take the places that are left; each workgroup of the others then adds half of
 // what it needs besides its steps.
-inline double kv4_time(int64_t whole, int64_t tiles, int q, int64_t steps, double bytes, int64_t rows, int64_t d,
-                       int64_t s) {
+//  * tiles that see `even` of the longest one's keys on average take that share of the rounds, and half
+//    a round at the end, but no less than the longest one alone.
+inline double kv4_time(int64_t whole, int64_t tiles, int q, int64_t steps, double even, double bytes, int64_t rows,
+                       int64_t d, int64_t s) {
   const int at = q == 1 ? 0 : (q == 2 ? 1 : 2);
   constexpr double kFixed[3] = {4300, 5500, 8000}, kWait[3] = {630, 650, 1080}, kBusy[3] = {400, 600, 830};
   constexpr int64_t kAtOnce[3] = {4 * 256, 2 * 256, 2 * 256};
@@ -65,9 +85,10 @@ inline double kv4_time(int64_t whole, int64_t tiles, int q, int64_t steps, doubl
   const double busy = kBusy[at] * (double)((here + 255) / 256);
   const double step = (kWait[at] > busy ? kWait[at] : busy) * (d == 128 ? 1.0 : 0.85);
   // (many rounds overlap, only their last one is not full)
-  const double rounds = units < 4 * kAtOnce[at] ? (double)((units + kAtOnce[at] - 1) / kAtOnce[at])
-                                                : (double)units / (double)kAtOnce[at] + 0.5;
-  const double ahead = (double)whole / (double)kAtOnce[at] * step * (double)((steps + kKv4Waves - 1) / kKv4Waves);
+  double rounds = (double)units * even / (double)kAtOnce[at] + 0.5;
+  if (even == 1.0 && units < 4 * kAtOnce[at]) rounds = (double)((units + kAtOnce[at] - 1) / kAtOnce[at]);
+  rounds = rounds > 1.0 ? rounds : 1.0;
+  const double ahead = even * (double)whole / (double)kAtOnce[at] * step * (double)((steps + kKv4Waves - 1) / kKv4Waves);
   const double wait = (step * (double)own + (whole > 0 ? 0.5 * kFixed[at] : 0.0)) * rounds + ahead, read = bytes / 5500.0;
   return kFixed[at] + (wait > read ? wait + 0.3 * read : read + 0.3 * wait) +
          (s > 1 ? 6000.0 + 25.0 * (double)s + 0.25 * (double)rows + (double)(rows * s * (d * 4 + 8) * 2) / 5000.0 : 0.0);
@@ -91,6 +112,23 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
       keys = span < keys ? span : keys;
     }
     const int64_t steps = (keys + kKv4StepKeys - 1) / kKv4StepKeys + 1;
+    // the average tile's steps, from 8 of them; 1 where all see the same keys
+    double even = 1.0;
+    if (row_tiles > 1 && chunk_len < cache_len) {
+      int64_t sum = 0;
+      constexpr int kSample = 8;
+      const int W = (int)(window < cache_len ? window : -1);
+      for (int i = 0; i < kSample; ++i) {
+        const int64_t row0 = (row_tiles * (2 * i + 1) / (2 * kSample)) * tile;
+        const int64_t last = row0 + tile < R ? row0 + tile - 1 : R - 1;
+        int lo, hi, none;
+        kv4_interval((int)(cache_len - nq + row0 / G), (int)cache_len, (int)chunk_len, W, &lo, &none);
+        kv4_interval((int)(cache_len - nq + last / G), (int)cache_len, (int)chunk_len, W, &none, &hi);
+        sum += hi > lo ? (hi - lo) / kKv4StepKeys + 1 : 0;
+      }
+      const double share = (double)sum / (double)(kSample * steps);
+      even = share < 0.9 ? share : 1.0;
+    }
     const double bytes = (double)(B * Hkv * keys * (d / 2 + d / 32) * 2) * (1.0 + 0.25 * (double)(row_tiles - 1));
     // all tiles split alike, or only those that would fill a last round in part
     const int64_t full = tiles / kAtOnce[q] * kAtOnce[q];
@@ -101,7 +139,7 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
       int n = 0;
       for (int s : kSplits) {
         if (s > 1 && (s > steps || rows * s * (d * 4 + 8) > kKv4MaxWorkspace)) break;
-        times[n] = kv4_time(whole, rest, q, steps, bytes, rows, d, s);
+        times[n] = kv4_time(whole, rest, q, steps, even, bytes, rows, d, s);
         least = n == 0 || times[n] < least ? times[n] : least;
         ++n;
       }

@@ -4,6 +4,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <random>
+#include <vector>
 
 #include "kv4_plan.h"
 
@@ -49,6 +50,26 @@ int main() {
     CHECK(lo == 0 && hi == n);
     kv4_interval(n - 1, n, n - 1, 0, &lo, &hi);
     CHECK(lo == n - 1 && hi == n);
+  }
+  // the order of a head's tiles: each of them once, the longest first, and every run of 32 with
+  // tiles from all over the head
+  for (int n = 1; n < 700; ++n) {
+    const int runs = kv4_runs(n);
+    std::vector<int> seen(n, 0), order(n);
+    for (int i = 0; i < n; ++i) {
+      order[i] = kv4_tile(i, n, runs);
+      CHECK(order[i] >= 0 && order[i] < n);
+      CHECK(seen[order[i]]++ == 0);
+    }
+    CHECK(order[0] == n - 1);
+    if (runs > 1)
+      for (int j = 0; j + n / runs <= n; ++j) {
+        double sum = 0;
+        for (int i = 0; i < n / runs; ++i) sum += order[j + i];
+        const double mean = sum / (n / runs), all = (n - 1) / 2.0;
+        CHECK(std::fabs(mean - all) <= 0.5 * runs + 0.5 * runs);
+      }
+    ++cases;
   }
   // plans: every step of every tile belongs to one workgroup, sizes and workspace agree
   long with_whole = 0;

@@ -59,6 +59,8 @@ CASES = [
     (2, 100, 2, 2, 64, 333, 7, 48, 2, FP32),           # rows of several chunks, from within one
     (1, 130, 3, 3, 128, 1111, 0, 130, -1, BF16),
     (1, 3, 64, 8, 128, 4000, 0, 1, -1, FP32),
+    (1, 1601, 4, 1, 64, 1601, 2, 1, -1, FP32),         # a hundred row tiles of one key head
+    (2, 1100, 4, 2, 128, 1203, 0, 60, 3, BF16),
 ]
 
 
@@ -75,20 +77,21 @@ def test_attn_parity(dev, case):
 
 
 @pytest.mark.parametrize("case", [
-    # B, Nq, H, Hkv, d, n, chunk_len, window, output type
-    (33, 1, 33, 33, 64, 1500, None, -1, FP32),
-    (1, 2100, 8, 2, 128, 5003, None, -1, BF16),
-    (1, 4300, 8, 1, 64, 4300, 700, 2, FP32),
-    (2, 2200, 8, 1, 128, 2600, 1, -1, FP32),
+    # B, Nq, H, Hkv, d, n, chunk_len, window, output type, whether tiles are split
+    (33, 1, 33, 33, 64, 1500, None, -1, FP32, True),
+    (1, 2100, 8, 2, 128, 5003, None, -1, BF16, True),
+    (1, 4300, 8, 1, 64, 4300, 700, 2, FP32, True),
+    (2, 2200, 8, 1, 128, 2600, 1, -1, FP32, False),
+    (1, 4300, 8, 1, 128, 4300, 1, -1, FP32, True),
 ], ids=lambda c: f"B{c[0]}q{c[1]}H{c[2]}of{c[3]}d{c[4]}n{c[5]}L{c[6]}W{c[7]}")
 def test_more_tiles_than_fit_at_once(dev, case):
     """One workgroup for the keys of most row tiles, several for those of the last ones: full
     lengths, and lengths that leave some workgroups without keys.  Where key heads are many, three are made
     and repeated; the oracle takes the first and the last sequence and one query head of each of their key heads."""
-    B, Nq, H, Hkv, d, n, L, W, ot = case
+    B, Nq, H, Hkv, d, n, L, W, ot, split = case
     print(f"\n[gpu case] kv4 attn, many tiles {case}", flush=True)
     ws = fastvr.kv4_attn_workspace(B, H, Hkv, Nq, d, n, L or n, W)
-    assert 0 < ws < B * H * Nq * (4 * d + 8)          # fewer than the rows have partial results
+    assert (ws > 0) == split and ws < B * H * Nq * (4 * d + 8)          # fewer than the rows have partial results
     made = min(Hkv, 3)
     _, cache, k, v = inputs(1, 1, made, made, d, n, n + 3, n + Nq)
     cache = fastvr.KV4Cache(*(t.repeat(B, Hkv // made, 1, 1) for t in cache))
