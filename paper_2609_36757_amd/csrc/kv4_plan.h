@@ -134,14 +134,20 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
     const int64_t full = tiles / kAtOnce[q] * kAtOnce[q];
     for (int tail = 0; tail < (full > 0 && full < tiles ? 2 : 1); ++tail) {
       const int64_t whole = tail ? full : 0, rest = tiles - whole, rows = rest * (row_tiles > 1 ? tile : R);
-      constexpr int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit};
-      double times[sizeof(kSplits) / sizeof(int)], least = 0;
+      // numbers of splits in general, and those that just fill one to four rounds
+      constexpr int kGeneral = 12, kFull = 4;
+      int64_t splits[kGeneral + kFull] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit};
+      for (int k = 1; k <= kFull; ++k) {
+        const int64_t s = k * kAtOnce[q] / rest;
+        splits[kGeneral + k - 1] = s < 1 ? 1 : (s > kKv4MaxSplit ? kKv4MaxSplit : s);
+      }
+      double times[kGeneral + kFull], least = 0;
       int n = 0;
-      for (int s : kSplits) {
-        if (s > 1 && (s > steps || rows * s * (d * 4 + 8) > kKv4MaxWorkspace)) break;
+      for (int64_t s : splits) {
+        if (s > 1 && (s > steps || rows * s * (d * 4 + 8) > kKv4MaxWorkspace)) continue;
         times[n] = kv4_time(whole, rest, q, steps, even, bytes, rows, d, s);
         least = n == 0 || times[n] < least ? times[n] : least;
-        ++n;
+        splits[n++] = s;
       }
       if (p.q_tiles != 0 && least >= best) continue;
       best = least;
@@ -149,8 +155,9 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
       p.row_tiles = row_tiles;
       // of splits that take the same time the most: shorter sequences than the longest leave
       // some of their workgroups nothing to do
-      while (times[n - 1] > (tail ? 1.0 : 1.03) * least) --n;
-      p.n_split = kSplits[n - 1];
+      p.n_split = 1;
+      for (int i = 0; i < n; ++i)
+        if (times[i] <= (tail ? 1.0 : 1.03) * least && splits[i] > p.n_split) p.n_split = (int32_t)splits[i];
       p.whole = p.n_split > 1 ? whole : tiles;
       p.rows = p.n_split > 1 ? rows : 0;
     }
