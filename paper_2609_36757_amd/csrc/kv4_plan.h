@@ -79,19 +79,20 @@ inline double kv4_time(int64_t whole, int64_t tiles, int q, int64_t steps, doubl
                        int64_t d, int64_t s) {
   const int at = q == 1 ? 0 : (q == 2 ? 1 : 2);
   constexpr double kFixed[3] = {4300, 5500, 8000}, kWait[3] = {630, 650, 1080}, kBusy[3] = {400, 600, 830};
-  constexpr int64_t kAtOnce[3] = {4 * 256, 2 * 256, 2 * 256};
-  const int64_t units = tiles * s, all = whole + units, here = all < kAtOnce[at] ? all : kAtOnce[at];
-  const int64_t own = ((steps + s - 1) / s + kKv4Waves - 1) / kKv4Waves;
+  const int64_t at_once = q == 1 ? 4 * 256 : 2 * 256;
+  const double rounds_each = q == 1 ? 1.0 / (4 * 256) : 1.0 / (2 * 256);
+  const int64_t units = tiles * s, all = whole + units, here = all < at_once ? all : at_once;
+  const uint32_t own = ((uint32_t)(steps + s - 1) / (uint32_t)s + kKv4Waves - 1) / kKv4Waves;
   const double busy = kBusy[at] * (double)((here + 255) / 256);
   const double step = (kWait[at] > busy ? kWait[at] : busy) * (d == 128 ? 1.0 : 0.85);
   // (many rounds overlap, only their last one is not full)
-  double rounds = (double)units * even / (double)kAtOnce[at] + 0.5;
-  if (even == 1.0 && units < 4 * kAtOnce[at]) rounds = (double)((units + kAtOnce[at] - 1) / kAtOnce[at]);
+  double rounds = (double)units * even * rounds_each + 0.5;
+  if (even == 1.0 && units < 4 * at_once) rounds = (double)((uint32_t)(units + at_once - 1) / (uint32_t)at_once);
   rounds = rounds > 1.0 ? rounds : 1.0;
-  const double ahead = even * (double)whole / (double)kAtOnce[at] * step * (double)((steps + kKv4Waves - 1) / kKv4Waves);
-  const double wait = (step * (double)own + (whole > 0 ? 0.5 * kFixed[at] : 0.0)) * rounds + ahead, read = bytes / 5500.0;
+  const double ahead = even * (double)whole * rounds_each * step * (double)((steps + kKv4Waves - 1) / kKv4Waves);
+  const double wait = (step * (double)own + (whole > 0 ? 0.5 * kFixed[at] : 0.0)) * rounds + ahead, read = bytes * (1.0 / 5500.0);
   return kFixed[at] + (wait > read ? wait + 0.3 * read : read + 0.3 * wait) +
-         (s > 1 ? 6000.0 + 25.0 * (double)s + 0.25 * (double)rows + (double)(rows * s * (d * 4 + 8) * 2) / 5000.0 : 0.0);
+         (s > 1 ? 6000.0 + 25.0 * (double)s + 0.25 * (double)rows + (double)(rows * s * (d * 4 + 8)) * (2.0 / 5000.0) : 0.0);
 }
 
 // B, H, Hkv, nq >= 1; 0 <= cache_len; 1 <= chunk_len; window >= -1; H a multiple of Hkv.
@@ -100,6 +101,19 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
   Kv4Plan p{};
   const int64_t G = H / Hkv, R = nq * G;
   constexpr int64_t kAtOnce[5] = {0, 4 * 256, 2 * 256, 0, 2 * 256};
+  // keys that a token sees on average, from 8 of them
+  double seen = (double)cache_len;
+  if (nq > 1 && chunk_len < cache_len) {
+    constexpr int kSample = 8;
+    const int W = (int)(window < cache_len ? window : -1);
+    int64_t sum = 0;
+    for (int i = 0; i < kSample; ++i) {
+      int lo, hi;
+      kv4_interval((int)(cache_len - nq + nq * (2 * i + 1) / (2 * kSample)), (int)cache_len, (int)chunk_len, W, &lo, &hi);
+      sum += hi - lo + kKv4StepKeys;
+    }
+    seen = (double)sum / kSample;
+  }
   double best = 0;
   for (int q : {4, 2, 1}) {
     if (q > 1 && R <= 8 * q) continue;  // half of the rows, and more, would be empty
@@ -112,23 +126,7 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
       keys = span < keys ? span : keys;
     }
     const int64_t steps = (keys + kKv4StepKeys - 1) / kKv4StepKeys + 1;
-    // the average tile's steps, from 8 of them; 1 where all see the same keys
-    double even = 1.0;
-    if (row_tiles > 1 && chunk_len < cache_len) {
-      int64_t sum = 0;
-      constexpr int kSample = 8;
-      const int W = (int)(window < cache_len ? window : -1);
-      for (int i = 0; i < kSample; ++i) {
-        const int64_t row0 = (row_tiles * (2 * i + 1) / (2 * kSample)) * tile;
-        const int64_t last = row0 + tile < R ? row0 + tile - 1 : R - 1;
-        int lo, hi, none;
-        kv4_interval((int)(cache_len - nq + row0 / G), (int)cache_len, (int)chunk_len, W, &lo, &none);
-        kv4_interval((int)(cache_len - nq + last / G), (int)cache_len, (int)chunk_len, W, &none, &hi);
-        sum += hi > lo ? (hi - lo) / kKv4StepKeys + 1 : 0;
-      }
-      const double share = (double)sum / (double)(kSample * steps);
-      even = share < 0.9 ? share : 1.0;
-    }
+    const double share = seen / (double)(keys + kKv4StepKeys), even = row_tiles > 1 && share < 0.9 ? share : 1.0;
     const double bytes = (double)(B * Hkv * keys * (d / 2 + d / 32) * 2) * (1.0 + 0.25 * (double)(row_tiles - 1));
     // all tiles split alike, or only those that would fill a last round in part
     const int64_t full = tiles / kAtOnce[q] * kAtOnce[q];
@@ -138,8 +136,8 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
       constexpr int kGeneral = 12, kFull = 4;
       int64_t splits[kGeneral + kFull] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, kKv4MaxSplit};
       for (int k = 1; k <= kFull; ++k) {
-        const int64_t s = k * kAtOnce[q] / rest;
-        splits[kGeneral + k - 1] = s < 1 ? 1 : (s > kKv4MaxSplit ? kKv4MaxSplit : s);
+        const int64_t s = rest > k * kAtOnce[q] ? 1 : (int64_t)((uint32_t)(k * kAtOnce[q]) / (uint32_t)rest);
+        splits[kGeneral + k - 1] = s < kKv4MaxSplit ? s : kKv4MaxSplit;
       }
       double times[kGeneral + kFull], least = 0;
       int n = 0;
