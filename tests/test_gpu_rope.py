@@ -100,6 +100,28 @@ def test_rope_views_in_place_and_rows_between(dev, layout, P):
     assert torch.equal(buf[:, :N, 2 * H:], before[:, :N, 2 * H:]) and torch.equal(buf[:, N:], before[:, N:])
 
 
+@pytest.mark.parametrize("d,P,dtype", [(128, 45, BF16), (64, 31, BF16), (128, 63, FP32), (64, 2, FP32)])
+def test_rope_in_place_of_odd_halves(dev, d, P, dtype):
+    """Halves whose second one starts anywhere, many tokens and a last head split that is not full."""
+    print(f"\n[gpu case] rope in place, odd halves {d} {P}", flush=True)
+    g = torch.Generator().manual_seed(P)
+    B, N, H = 2, 3001, 7
+    x = torch.randn((B, N, H, d), generator=g).to(dtype).to(dev)
+    f, _ = fastvr.rope_inv_freq(P)
+    ft = torch.tensor(f, dtype=torch.float64, device=dev)
+    pos = torch.randint(0, 50000, (B, N), generator=g, dtype=torch.int32).to(dev)
+    want = fastvr.rope(x, pos, ft, layout="half")
+    check(want, x, pos, f, "half", None, 1.0, False)
+    before = x.clone()
+    x[0, 5, 3, 2 * P:] = float("inf")          # elements that pass stay what they are
+    got = fastvr.rope(x, pos, ft, layout="half", out=x)
+    torch.cuda.synchronize()
+    assert got.data_ptr() == x.data_ptr()
+    assert torch.isinf(x[0, 5, 3, 2 * P:]).all()
+    x[0, 5, 3, 2 * P:] = before[0, 5, 3, 2 * P:]
+    assert torch.equal(x, want)
+
+
 def test_rope_non_finite_values_stay_in_their_pair(dev):
     print("\n[gpu case] rope NaN and infinity", flush=True)
     x = torch.zeros((1, 3, 2, 64), dtype=BF16, device=dev)
