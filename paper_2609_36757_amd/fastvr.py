@@ -487,10 +487,10 @@ def tile_blend(tiles, Hg: int, Wg: int, *, tile: int = 64, overlap: int = 16, z_
 # The checks below are on the path of calls whose kernels take 3 to 10 us, so the usual
 # case is decided with few calls into torch (0.05 to 0.1 us each): contiguous tensors, one device.
 
-def _view_strides(t, name):
-    """_bnhd_strides with the strides of axes of one element, which torch leaves to
-    chance, as if the view were contiguous there."""
-    B, N, H, d = t.shape
+def _view_strides(t, name, shape):
+    """_bnhd_strides, of a view of that shape, with the strides of axes of one element, which
+    torch leaves to chance, as if the view were contiguous there."""
+    B, N, H, d = shape
     if t.is_contiguous():
         return N * H * d, H * d
     sb, st, sh, sd = t.stride()
@@ -504,12 +504,14 @@ def _view_strides(t, name):
 
 
 def _check_view(t, name, shape, dtype):
-    """Strides of a [B, N, H, d] view of that shape and dtype."""
+    """Strides of a [B, N, H, d] view of that shape (None: its own, known to have four axes) and dtype."""
     if t.dtype is not dtype or not t.is_cuda:
         raise ValueError(f"{name} must be a {str(dtype).split('.')[1]} GPU tensor")
-    if t.shape != shape:
+    if shape is None:
+        shape = t.shape
+    elif t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
-    return _view_strides(t, name)
+    return _view_strides(t, name, shape)
 
 
 def _stream_on(device: int, stream, *tensors):
@@ -533,16 +535,22 @@ def _stream_on(device: int, stream, *tensors):
 
 
 def _empty(like, shape, dtype, stream=None):
-    """A contiguous tensor on like's device (empty_like: 0.9 us against 1.5), for the stream that takes
-    the call: torch's allocator hands memory out and takes it back in the order of one stream, and a
-    workspace made here goes back as soon as the call has returned."""
-    import torch
+    """A contiguous tensor on like's device, for the stream that takes the call: torch's allocator hands
+    memory out and takes it back in the order of one stream, and a workspace made here goes back
+    as soon as the call has returned."""
     if stream is not None:
+        import torch
         with torch.cuda.stream(stream):
-            return _empty(like, shape, dtype)
-    if like.dtype is dtype and like.shape == shape and like.is_contiguous():
-        return torch.empty_like(like)
+            return like.new_empty(shape, dtype=dtype)
     return like.new_empty(shape, dtype=dtype)
+
+
+def _empty_as(like, shape, dtype, stream):
+    """_empty of like's own shape (empty_like: 1.1 us against 1.5)."""
+    if stream is None and like.dtype is dtype and like.is_contiguous():
+        import torch
+        return torch.empty_like(like)
+    return _empty(like, shape, dtype, stream)
 
 
 def rope_inv_freq(n_pairs: int, *, base: float = 10000.0, sections=None, scaling: str | None = None,
@@ -590,7 +598,7 @@ def _rope(x, positions, inv_freq, layout, sections, amplitude, out, out_dtype, i
     shape = x.shape
     B, N, H, d = shape
     x32 = x.dtype is fp32
-    xs = _check_view(x, "x", shape, fp32 if x32 else bf16)
+    xs = _check_view(x, "x", None, fp32 if x32 else bf16)
     if layout not in ("interleaved", "half"):
         raise ValueError(f"layout must be 'interleaved' or 'half', got {layout!r}")
     if inv_freq.dtype is not torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
@@ -620,7 +628,7 @@ def _rope(x, positions, inv_freq, layout, sections, amplitude, out, out_dtype, i
     handle = _stream_on(x.get_device(), stream, positions, inv_freq, out)
     ys = (N * H * d, H * d)
     if out is None:
-        out = _empty(x, shape, out_dtype, stream)
+        out = _empty_as(x, shape, out_dtype, stream)
     else:
         ys = _check_view(out, "out", shape, out_dtype)
     status = load().fastvr_rope(x.data_ptr(), *xs, 1 if x32 else 0, out.data_ptr(), *ys,
@@ -694,9 +702,9 @@ def _check_kv4(cache):
 
 
 def _check_int32(t, name, n):
-    import torch
     if t is None:
         return None
+    import torch
     if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 GPU tensor [{n}]")
     return t.data_ptr()
@@ -736,7 +744,7 @@ def kv4_read(cache, n: int, first: int = 0, *, starts=None, k_out=None, v_out=No
     else:
         ks = _check_view(k_out, "k_out", shape, torch.bfloat16)
     if v_out is None:
-        v_out = _empty(k_out, shape, torch.bfloat16, stream)
+        v_out = _empty_as(k_out, shape, torch.bfloat16, stream)
     else:
         vs = _check_view(v_out, "v_out", shape, torch.bfloat16)
     sp = _check_int32(starts, "starts", B)
@@ -774,7 +782,7 @@ def kv4_attn(q, cache, cache_len: int, *, lens=None, chunk_len: int | None = Non
     _, Nq, H, _ = shape
     if shape[0] != B or shape[3] != d:
         raise ValueError(f"shape mismatch: q {tuple(shape)}, cache of {B} sequences and head_dim {d}")
-    qs = _check_view(q, "q", shape, bf16)
+    qs = _check_view(q, "q", None, bf16)
     if chunk_len is None:
         chunk_len = max(cache_len, 1)
     if scale is None:
@@ -786,7 +794,7 @@ def kv4_attn(q, cache, cache_len: int, *, lens=None, chunk_len: int | None = Non
     handle = _stream_on(q.get_device(), stream, *cache, lens, out, lse, workspace)
     os_ = (Nq * H * d, H * d)
     if out is None:
-        out = _empty(q, shape, out_dtype, stream)
+        out = _empty_as(q, shape, out_dtype, stream)
     else:
         os_ = _check_view(out, "out", shape, out_dtype)
     if lse is not None:
