@@ -34,11 +34,11 @@
 // What bounds it.  One row tile (a token of each sequence): the cache's bytes; a
 // step's 4.3 KB take longer than its 190 vector instructions and 256 cycles of matrix
 // core.  One query over 65280 keys of 12 heads: 20.7 us for 107 MB (5.1 TB/s, a copy's
-// rate), and 4 us for the join.  Four row tiles: conversion, exp2 and sums, 240 vector
-// instructions a step of 64 rows against 1024 cycles of matrix core; two waves of a
-// SIMD overlap them to 56% of the matrix core's time.  16320 queries over 65280 keys:
-// 5.1 ms, 1280 TFLOP/s (a large bf16 GEMM reaches 1500 on the same card, the bf16
-// forward on an expanded cache 1300).  What it took: Q in LDS and V's scales loaded
+// rate), and 4 us for the join.  Four row tiles: conversion, exp2 and sums, 270 vector
+// instructions a step of 64 rows, which two waves of a SIMD overlap with 1024 cycles of
+// matrix core (busy 56% of the cycles under the profiler, where a call takes 15% longer).
+// 16320 queries over 65280 keys of 12 heads: 5.1 to 5.4 ms by card, 1210 to 1290 TFLOP/s
+// (a large bf16 GEMM reaches 1500, the bf16 forward on an expanded cache 1300).  What it took: Q in LDS and V's scales loaded
 // late, for two waves on a SIMD without a spilled register (15.9 ms with one wave on a
 // SIMD; 5.6 with two); products at a higher wave priority (5.4); V converted and
 // paired between the products (5.1).
