@@ -116,6 +116,28 @@ __device__ __forceinline__ float row_sum4(float x) {
   return x + o;
 }
 
+// maximum and sum over a wave's lanes
+template <int CTRL>
+__device__ __forceinline__ float row_move(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+constexpr int kQuad1032 = 0xB1, kQuad2301 = 0x4E, kRowRor4 = 0x124, kRowRor8 = 0x128;
+__device__ __forceinline__ float wave_max(float x) {
+  x = __builtin_fmaxf(x, row_move<kQuad1032>(x));
+  x = __builtin_fmaxf(x, row_move<kQuad2301>(x));
+  x = __builtin_fmaxf(x, row_move<kRowRor4>(x));
+  x = __builtin_fmaxf(x, row_move<kRowRor8>(x));
+  return row_max4(x);
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  x += row_move<kQuad1032>(x);
+  x += row_move<kQuad2301>(x);
+  x += row_move<kRowRor4>(x);
+  x += row_move<kRowRor8>(x);
+  x = row_sum4(x);  // (lanes add in different orders: one of them for all)
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x)));
+}
+
 template <int D>
 struct Step {  // what a lane loads for 32 keys
   static constexpr int kK = D / 32;   // dwords of K a lane holds per key
@@ -558,17 +580,14 @@ __global__ __launch_bounds__(kThreads) void kv4_join_kernel(const Kv4Params p) {
   const float* ml = p.part + p.rows * p.n_split * D + row * p.n_split * 2;
   const float m_s = lane < p.n_split ? ml[2 * lane] : kNone;
   const float l_s = lane < p.n_split ? ml[2 * lane + 1] : 0.f;
-  float m = m_s;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+  const float m = wave_max(m_s);
   const float f = __builtin_amdgcn_exp2f(m_s - m);
-  float sum = l_s * f;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+  const float sum = wave_sum(l_s * f);
   float v[kE] = {};
 #pragma unroll
   for (int k = 0; k < kMine; ++k) {
-    const float w = __shfl(f, k * WAVES + first);
+    const float w =
+        __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), k * WAVES + first));
 #pragma unroll
     for (int j = 0; j < kE; ++j) v[j] += w * x[k][j];
   }
