@@ -376,6 +376,8 @@ fastvr_status fastvr_kv4_read(const void* k_codes, const void* k_scales, const v
  *              fastvr_kv4_attn_workspace gives for these sizes (may be NULL for 0);
  *              the call's own until its work on `stream` has ended
  * Results do not depend on the workspace's contents; equal calls give equal bits.
+ * Scores, LSE and all sums are fp32; the softmax weights are held to 2^-16 of themselves
+ * where o is fp32, and may be rounded to bf16 (to 2^-8) where o is.
  *
  * Preconditions (else FASTVR_ERR_INVALID_ARGUMENT unless noted): sizes >= 0; d in
  * {64, 128}; H a multiple of Hkv; 0 <= cache_len <= capacity; chunk_len >= 1;

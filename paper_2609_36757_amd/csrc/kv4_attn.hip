@@ -24,15 +24,20 @@
 //  * The maximum a row is measured against is raised only when a score exceeds it by
 //    8 (in log2 units: P <= 2^8 then), so that most steps need no exchange between
 //    lanes and no rescale of O.
-// What is rounded: P to bf16 for the products (half a step, 2^-8 of each weight; the
-// sums l and all of S, LSE and O are fp32), and O where bf16 is asked for.  K and V
-// are exact in bf16, so their products with Q and P are exact.  (The matrix
+// What is rounded: P enters the products as a sum of two bf16 numbers, the second one
+// the rest of the first one's rounding, so a weight is off by 2^-16 of itself; with four row
+// tiles and O in bf16 as one, off by half a step, 2^-8, which is the rounding that the caller
+// asks of O.  (The second part takes half as many matrix instructions again: 16320 queries
+// over 65280 keys of 12 heads 5.0 ms with one part, 6.9 with two; where few rows leave the
+// matrix core idle it costs little: one query 22.6 and 23.1 us, 1024 tokens that see the
+// ones before them, two row tiles, 14.6 and 16.4 us.)  The sums l and all of S, LSE and O are fp32, and O is
+// rounded where bf16 is asked for.  K and V are exact in bf16, so their products with Q and P are exact.  (The matrix
 // instruction that takes 4-bit operands and block scales itself would save K's
 // conversion, with Q in two 8-bit parts; its sums were off by 4e-5 of the largest, too
 // much for LSE.)
 //
 // What bounds it.  One row tile (a token of each sequence): the cache's bytes; a
-// step's 4.3 KB take longer than its 190 vector instructions and 256 cycles of matrix
+// step's 4.3 KB take longer than its 210 vector instructions and 384 cycles of matrix
 // core.  One query over 65280 keys of 12 heads: 20.7 us for 107 MB (5.1 TB/s, a copy's
 // rate), and 4 us for the join.  Four row tiles: conversion, exp2 and sums, 270 vector
 // instructions a step of 64 rows, which two waves of a SIMD overlap with 1024 cycles of
@@ -355,7 +360,8 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
   };
 
   // Step st; the loads of step nx take the place of what has been used.
-  auto step = [&](int st, int nx, bool masked) {
+  auto step = [&](int st, int nx, bool masked, auto parts) {
+    constexpr bool kTwo = decltype(parts)::value == 2;  // P as a sum of two bf16 numbers
     __builtin_amdgcn_s_setprio(1);
     const uint32_t q_lane = opaque(lane);  // (Q in LDS is read anew in each step)
     f32x4 sc[QT][2];
@@ -402,10 +408,10 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
         for (int j = 0; j < kE; ++j) acc[t][j] *= alpha;
       }
     }
-    u32x4 pf[QT];
+    u32x4 pf[QT], rest[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      bf16x8 pb;
+      bf16x8 pb, pr;
       float sum = 0.f;
 #pragma unroll
       for (int x = 0; x < 2; ++x)
@@ -414,9 +420,11 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
           const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][x][r], p.c, -mc[t]));  // 0 where masked
           sum += e;
           pb[4 * x + r] = (__bf16)e;
+          if (kTwo) pr[4 * x + r] = (__bf16)(e - (float)pb[4 * x + r]);
         }
       l[t] += sum;
       pf[t] = __builtin_bit_cast(u32x4, pb);
+      if (kTwo) rest[t] = __builtin_bit_cast(u32x4, pr);
     }
     if (QT > 2) __builtin_amdgcn_sched_barrier(0);  // one phase's registers at a time
     // V: keys 4 g + (0..3) and 16 + 4 g + (0..3), elements n * kE ..; two elements of the 8
@@ -435,15 +443,23 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
       uint32_t w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] = kv4_pair<P>(code[i], v_scale[i]);
+      u32x4 a[2];
 #pragma unroll
-      for (int j = 2 * P; j < 2 * P + 2; ++j) {
-        u32x4 a;
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          a[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], (j & 1) ? 0x07060302u : 0x05040100u);
+          a[j][i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], j ? 0x07060302u : 0x05040100u);
+      // (one tile: an accumulator's two products are not neighbours)
+      constexpr int kAtOnce = QT == 1 ? 2 : 1;
 #pragma unroll
-        for (int t = 0; t < QT; ++t) acc[t][j] = mfma16(a, pf[t], acc[t][j]);
-      }
+      for (int j0 = 0; j0 < 2; j0 += kAtOnce)
+#pragma unroll
+        for (int part = 0; part < (kTwo ? 2 : 1); ++part)
+#pragma unroll
+          for (int j = j0; j < j0 + kAtOnce; ++j)
+#pragma unroll
+            for (int t = 0; t < QT; ++t)
+              acc[t][2 * P + j] = mfma16(a[j], part == 0 ? pf[t] : rest[t], acc[t][2 * P + j]);
     };
     two(std::integral_constant<int, 0>{});
     two(std::integral_constant<int, 1>{});
@@ -454,7 +470,7 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
     __builtin_amdgcn_sched_group_barrier(SCHED_VALU, 32, 0);
 #pragma unroll
     for (int i = 0; i < QT * kE; ++i) {
-      __builtin_amdgcn_sched_group_barrier(SCHED_MFMA, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(SCHED_MFMA, kTwo ? 2 : 1, 0);
       __builtin_amdgcn_sched_group_barrier(SCHED_VALU, 8 / QT, 0);
     }
   };
@@ -469,8 +485,14 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
       s.vs[i] = opaque(s.vs[i]);
     }
   }
-  for (; st < end; st += kKv4Waves)  // (the last step loads itself once more)
-    step(st, st + kKv4Waves < end ? st + kKv4Waves : st, st < in_lo || st >= in_hi);
+  // (two loops one behind the other, of which one runs: as the two sides of a branch they spill)
+  const int one_end = __builtin_amdgcn_readfirstlane(QT == 4 && p.o_bf16 ? end : 0);
+  // (the last step loads itself once more)
+  if (QT == 4)
+    for (; st < one_end; st += kKv4Waves)
+      step(st, st + kKv4Waves < end ? st + kKv4Waves : st, st < in_lo || st >= in_hi, std::integral_constant<int, 1>{});
+  for (; st < end; st += kKv4Waves)
+    step(st, st + kKv4Waves < end ? st + kKv4Waves : st, st < in_lo || st >= in_hi, std::integral_constant<int, 2>{});
 
   // join the waves
 #pragma unroll
