@@ -647,11 +647,13 @@ fastvr_status kv4_copy(bool write, const void* kc, const void* ks, const void* v
         if (t.bytes[a] > 0 && overlap(t.ptr[a], t.bytes[a], t.ptr[b], t.bytes[b]))
           return fail(FASTVR_ERR_INVALID_ARGUMENT, "%s overlaps %s", kKv4Names[a], kKv4Names[b]);
   } else {
-    // K and V side by side in one token row (views of one buffer) interleave without overlap
+    // K and V side by side in one token row (views of one buffer) interleave without overlap; of one
+    // token a sequence the rows are a batch stride apart, and the token strides mean nothing
     const char *kp = static_cast<const char*>(k), *vp = static_cast<const char*>(v);
     const uintptr_t gap = kp < vp ? uintptr_t(vp - kp) : uintptr_t(kp - vp);
-    const bool beside = k_st == v_st && (B == 1 || k_sb == v_sb) && gap >= uintptr_t(hd * 2) &&
-                        gap + uintptr_t(hd * 2) <= uintptr_t(k_st * 2);
+    const int64_t row = n == 1 ? k_sb : k_st;
+    const bool beside = (n == 1 || k_st == v_st) && (B == 1 || k_sb == v_sb) && gap >= uintptr_t(hd * 2) &&
+                        gap + uintptr_t(hd * 2) <= uintptr_t(row * 2);
     if (!beside && overlap(k, kb, v, vb)) return fail(FASTVR_ERR_INVALID_ARGUMENT, "k_out overlaps v_out");
     if (sb > 0 && (overlap(starts, sb, k, kb) || overlap(starts, sb, v, vb)))
       return fail(FASTVR_ERR_INVALID_ARGUMENT, "starts overlaps k_out or v_out");
