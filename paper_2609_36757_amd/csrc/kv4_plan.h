@@ -127,7 +127,8 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
     }
     const int64_t steps = (keys + kKv4StepKeys - 1) / kKv4StepKeys + 1;
     const double share = seen / (double)(keys + kKv4StepKeys), even = row_tiles > 1 && share < 0.9 ? share : 1.0;
-    const double bytes = (double)(B * Hkv * keys * (d / 2 + d / 32) * 2) * (1.0 + 0.25 * (double)(row_tiles - 1));
+    // (in double from the start: of sizes that the caller refuses afterwards the product passes 2^63)
+    const double bytes = (double)(B * Hkv) * (double)(keys * (d / 2 + d / 32) * 2) * (1.0 + 0.25 * (double)(row_tiles - 1));
     // all tiles split alike, or only those that would fill a last round in part
     const int64_t full = tiles / kAtOnce[q] * kAtOnce[q];
     for (int tail = 0; tail < (full > 0 && full < tiles ? 2 : 1); ++tail) {
