@@ -3,10 +3,13 @@
     python -m paper_2609_36757_amd.build
 
 Every HIP source is compiled with packed-FP32 instruction selection disabled
-(``-target-feature -packed-fp32-ops``)."""
+(``-target-feature -packed-fp32-ops``).  A build with a kernel that spills vector registers or
+uses scratch memory is refused: an attention kernel that spilled accumulators gave wrong sums in
+some lanes (a reload under a partial execution mask), besides being slow."""
 from __future__ import annotations
 
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -37,16 +40,32 @@ def compile_cmd(out: str) -> list[str]:
             *[os.path.join(CSRC, s) for s in SOURCES], "-o", out]
 
 
+RESOURCES = "-Rpass-analysis=kernel-resource-usage"  # what each kernel takes, as remarks
+
+
+def spilling(remarks: str) -> list[str]:
+    """The kernels that spill vector registers or use scratch memory, from the compiler's remarks."""
+    bad = []
+    for kernel in remarks.split("remark: Function Name: ")[1:]:
+        used = re.findall(r"(?: VGPRs Spill|ScratchSize \[bytes/lane\]): (\d+)", kernel)
+        if any(int(n) for n in used):
+            bad.append(kernel.split()[0])
+    return bad
+
+
 def build(verbose: bool = False) -> str:
     tmp = LIB_PATH + f".tmp{os.getpid()}"
-    cmd = compile_cmd(tmp)
+    cmd = compile_cmd(tmp) + [RESOURCES]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
+    spills = spilling(res.stderr)
+    if res.returncode != 0 or spills:
         if os.path.exists(tmp):
             os.unlink(tmp)
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{res.stdout}\n{res.stderr}")
+        if res.returncode != 0:
+            raise RuntimeError(f"hipcc failed ({res.returncode}):\n{res.stdout}\n{res.stderr}")
+        raise RuntimeError(f"kernels that spill vector registers or use scratch memory: {', '.join(spills)}")
     os.replace(tmp, LIB_PATH)
     return LIB_PATH
 
