@@ -566,7 +566,7 @@ def rope_inv_freq(n_pairs: int, *, base: float = 10000.0, sections=None, scaling
     * ``"ntk"``: base * factor^(n / (n - 1)), which keeps the fastest pair and divides the slowest by ``factor``;
     * ``"yarn"`` (arXiv 2309.00071): pairs that turn ``fast`` times or more within original_len
       are kept, those that turn ``slow`` times or less divided by ``factor``, the ones between
-      blended linearly in their turns; amplitude 0.1 ln(factor) + 1."""
+      blended linearly in their turns; amplitude 0.1 ln(factor) + 1; factor >= 1."""
     if n_pairs < 0 or not base > 0 or not factor > 0:
         raise ValueError("need n_pairs >= 0, base > 0 and factor > 0")
     if sections is not None:
@@ -583,8 +583,8 @@ def rope_inv_freq(n_pairs: int, *, base: float = 10000.0, sections=None, scaling
     if scaling == "linear":
         return [f / factor for f in freq], 1.0
     if scaling == "yarn":
-        if original_len < 1 or not fast > slow:
-            raise ValueError("yarn needs original_len >= 1 and fast > slow")
+        if original_len < 1 or not fast > slow or not 1 <= factor < math.inf:
+            raise ValueError("yarn needs original_len >= 1, fast > slow and a finite factor >= 1")
         keep = [min(1.0, max(0.0, (original_len * f / (2 * math.pi) - slow) / (fast - slow))) for f in freq]
         return [f * k + f / factor * (1 - k) for f, k in zip(freq, keep)], 0.1 * math.log(factor) + 1.0
     return freq, 1.0
