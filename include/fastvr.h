@@ -328,6 +328,9 @@ fastvr_status fastvr_rope(const void* x, int64_t x_sb, int64_t x_st, int32_t x_f
  * each element goes to the nearest value, ties to the even code.  A block that holds an
  * infinity or NaN stands for NaN (byte 255, codes 0).  The values that codes and
  * scales stand for are exact in bf16.
+ * A new cache is zeros, which stand for zeros.  Append writes no other scale bytes than
+ * these; what a block with byte 0 or 1 and codes that are not zero, or with byte 253 or
+ * 254, stands for is undefined to the calls that see it.
  *
  * fastvr_kv4_append: n_new rows of K and V (bf16 [B, n_new, H, d] views) go to
  * token rows first .. first + n_new - 1 of every sequence, or, when starts (int32
