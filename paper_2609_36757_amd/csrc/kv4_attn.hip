@@ -649,8 +649,7 @@ hipError_t launch_t(const Kv4Params& p, const Kv4Plan& plan, hipStream_t stream)
   if (plan.n_split > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    // a wave a row where that fills the chip
-    if (plan.n_split <= 16 && plan.rows >= 2048)
+    if (kv4_join_waves(plan) == 1)
       hipLaunchKernelGGL((kv4_join_kernel<D, 1>), dim3((unsigned)((plan.rows + kKv4Waves - 1) / kKv4Waves)), block, 0, stream,
                          p);
     else

@@ -167,4 +167,8 @@ inline Kv4Plan kv4_plan(int64_t B, int64_t H, int64_t Hkv, int64_t nq, int64_t d
   return p;
 }
 
+// Waves that join a row's shares: a workgroup of four for a row, or, where a wave a row fills the
+// chip and holds all of a row's shares, one.
+inline int kv4_join_waves(const Kv4Plan& p) { return p.n_split <= 16 && p.rows >= 2048 ? 1 : kKv4Waves; }
+
 }  // namespace fastvr
