@@ -25,28 +25,30 @@
 //    8 (in log2 units: P <= 2^8 then), so that most steps need no exchange between
 //    lanes and no rescale of O.
 // What is rounded: P enters the products as a sum of two bf16 numbers, the second one
-// the rest of the first one's rounding, so a weight is off by 2^-16 of itself; with four row
-// tiles and O in bf16 as one, off by half a step, 2^-8, which is the rounding that the caller
-// asks of O.  (The second part takes half as many matrix instructions again: 16320 queries
-// over 65280 keys of 12 heads 5.0 ms with one part, 6.9 with two; where few rows leave the
-// matrix core idle it costs little: one query 22.6 and 23.1 us, 1024 tokens that see the
-// ones before them, two row tiles, 14.6 and 16.4 us.)  The sums l and all of S, LSE and O are fp32, and O is
-// rounded where bf16 is asked for.  K and V are exact in bf16, so their products with Q and P are exact.  (The matrix
-// instruction that takes 4-bit operands and block scales itself would save K's
-// conversion, with Q in two 8-bit parts; its sums were off by 4e-5 of the largest, too
-// much for LSE.)
+// the rest of the first one's rounding, so a weight is off by 2^-16 of itself; with four
+// row tiles and O in bf16 as one, off by half a step, 2^-8, the rounding that the caller
+// asks of O.  (The second part takes half as many matrix instructions again and 20 vector
+// instructions a row tile: 16320 queries over 65280 keys of 12 heads 5.1 ms with one part,
+// 6.9 with two.  Where rows are few it costs little: one query over 65280 keys 22.9 and
+// 23.2 us; one row tile a workgroup with all CUs full, 1024 tokens that see the ones before
+// them, 14.7 and 16.1; two, 32 queries over 65280 keys, 26.2 and 28.8.)  The sums l and all of
+// S, LSE and O are fp32, and O is rounded where bf16 is asked for.  K and V are exact in
+// bf16, so their products with Q and P are exact.  (The matrix instruction that takes
+// 4-bit operands and block scales itself would save K's conversion, with Q in two 8-bit
+// parts; its sums were off by 4e-5 of the largest, too much for LSE.)
 //
-// What bounds it.  One row tile (a token of each sequence): the cache's bytes; a
-// step's 4.3 KB take longer than its 210 vector instructions and 384 cycles of matrix
-// core.  One query over 65280 keys of 12 heads: 20.7 us for 107 MB (5.1 TB/s, a copy's
-// rate), and 4 us for the join.  Four row tiles: conversion, exp2 and sums, 270 vector
-// instructions a step of 64 rows, which two waves of a SIMD overlap with 1024 cycles of
-// matrix core (busy 56% of the cycles under the profiler, where a call takes 15% longer).
-// 16320 queries over 65280 keys of 12 heads: 5.1 to 5.4 ms by card, 1210 to 1290 TFLOP/s
-// (a large bf16 GEMM reaches 1500, the bf16 forward on an expanded cache 1300).  What it took: Q in LDS and V's scales loaded
-// late, for two waves on a SIMD without a spilled register (15.9 ms with one wave on a
-// SIMD; 5.6 with two); products at a higher wave priority (5.4); V converted and
-// paired between the products (5.1).
+// What bounds it.  One row tile (a token of each sequence): the cache's bytes; a step's
+// 4.3 KB take longer than its 205 vector instructions and 384 cycles of matrix core.  One
+// query over 65280 keys of 12 heads: 20.2 us for 107 MB (5.3 TB/s, a copy's rate), and 4
+// us for the join.  Four row tiles: the issue of vector instructions (conversion, exp2,
+// sums: 265 a step of 64 rows, beside 64 matrix instructions of 16 cycles).  Over 16320
+// queries and 65280 keys of 12 heads vector and matrix instructions issue in 78% of the
+// cycles and the matrix cores are busy in 56% (under the profiler, where a call takes 10%
+// longer); 80% and 38% with head_dim 64.  That call takes 5.0 to 5.5 ms by card, 1190 to 1310
+// TFLOP/s (a large bf16 GEMM reaches 1500, the bf16 forward on an expanded cache 1300).  What it took: Q in
+// LDS and V's scales loaded late, for two waves on a SIMD without a spilled register (15.9 ms
+// with one wave on a SIMD; 5.6 with two); products at a higher wave priority (5.4); V
+// converted and paired between the products (5.1).
 //
 // Keys a row does not see: their P is zero, and in the steps where that can happen
 // V blocks that are not finite (rows behind a sequence may hold anything) are taken
@@ -411,20 +413,25 @@ __global__ __launch_bounds__(kThreads, QT == 1 ? 4 : 2) void kv4_attn_kernel(con
     u32x4 pf[QT], rest[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-      bf16x8 pb, pr;
-      float sum = 0.f;
+      float e[8], sum = 0.f;
+      bf16x8 pb;
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][x][r], p.c, -mc[t]));  // 0 where masked
-          sum += e;
-          pb[4 * x + r] = (__bf16)e;
-          if (kTwo) pr[4 * x + r] = (__bf16)(e - (float)pb[4 * x + r]);
-        }
+      for (int i = 0; i < 8; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][i >> 2][i & 3], p.c, -mc[t]));  // 0 where masked
+        sum += e[i];
+        pb[i] = (__bf16)e[i];
+      }
       l[t] += sum;
       pf[t] = __builtin_bit_cast(u32x4, pb);
-      if (kTwo) rest[t] = __builtin_bit_cast(u32x4, pr);
+      if (kTwo) {
+        // (from the packed pairs: of single elements the compiler converts each once more)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint32_t pair = pf[t][i >> 1];
+          pb[i] = (__bf16)(e[i] - __builtin_bit_cast(float, (i & 1) ? pair & 0xffff0000u : pair << 16));
+        }
+        rest[t] = __builtin_bit_cast(u32x4, pb);
+      }
     }
     if (QT > 2) __builtin_amdgcn_sched_barrier(0);  // one phase's registers at a time
     // V: keys 4 g + (0..3) and 16 + 4 g + (0..3), elements n * kE ..; two elements of the 8
