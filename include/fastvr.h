@@ -328,9 +328,8 @@ fastvr_status fastvr_rope(const void* x, int64_t x_sb, int64_t x_st, int32_t x_f
  * each element goes to the nearest value, ties to the even code.  A block that holds an
  * infinity or NaN stands for NaN (byte 255, codes 0).  The values that codes and
  * scales stand for are exact in bf16.
- * A new cache is zeros, which stand for zeros.  Append writes no other scale bytes than
- * these; what a block with byte 0 or 1 and codes that are not zero, or with byte 253 or
- * 254, stands for is undefined to the calls that see it.
+ * Zeros, as of a new cache, stand for zeros.  What other blocks with byte 0 or 1, or any
+ * with 253 or 254, stand for is undefined to the calls that see them; append writes none.
  *
  * fastvr_kv4_append: n_new rows of K and V (bf16 [B, n_new, H, d] views) go to
  * token rows first .. first + n_new - 1 of every sequence, or, when starts (int32
@@ -380,7 +379,8 @@ fastvr_status fastvr_kv4_read(const void* k_codes, const void* k_scales, const v
  *              the call's own until its work on `stream` has ended
  * Results do not depend on the workspace's contents; equal calls give equal bits.
  * Scores, LSE and all sums are fp32; the softmax weights are held to 2^-16 of themselves
- * where o is fp32, and may be rounded to bf16 (to 2^-8) where o is.
+ * where o is fp32, and may be rounded to bf16 (to 2^-8) where o is.  The scores of keys that a
+ * row sees stay below 2e38 in magnitude (fp32's range, in base 2).
  *
  * Preconditions (else FASTVR_ERR_INVALID_ARGUMENT unless noted): sizes >= 0; d in
  * {64, 128}; H a multiple of Hkv; 0 <= cache_len <= capacity; chunk_len >= 1;

@@ -38,14 +38,14 @@
 // parts; its sums were off by 4e-5 of the largest, too much for LSE.)
 //
 // What bounds it.  One row tile (a token of each sequence): the cache's bytes; a step's
-// 4.3 KB take longer than its 205 vector instructions and 384 cycles of matrix core.  One
+// 4.3 KB take longer than its 220 vector instructions and 384 cycles of matrix core.  One
 // query over 65280 keys of 12 heads: 20.2 us for 107 MB (5.3 TB/s, a copy's rate), and 4
 // us for the join.  Four row tiles: the issue of vector instructions (conversion, exp2,
 // sums: 265 a step of 64 rows, beside 64 matrix instructions of 16 cycles).  Over 16320
-// queries and 65280 keys of 12 heads vector and matrix instructions issue in 78% of the
-// cycles and the matrix cores are busy in 56% (under the profiler, where a call takes 10%
-// longer); 80% and 38% with head_dim 64.  That call takes 5.0 to 5.5 ms by card, 1190 to 1310
-// TFLOP/s (a large bf16 GEMM reaches 1500, the bf16 forward on an expanded cache 1300).  What it took: Q in
+// queries and 65280 keys of 12 heads vector and matrix instructions issue in 80% of the
+// cycles and the matrix cores are busy in 57% (under the profiler, where a call takes 10%
+// longer); 81% and 38% with head_dim 64.  That call takes 5.0 to 5.7 ms by card and scores, 1140 to
+// 1310 TFLOP/s (a large bf16 GEMM reaches 1500, the bf16 forward on an expanded cache 1300).  What it took: Q in
 // LDS and V's scales loaded late, for two waves on a SIMD without a spilled register (15.9 ms
 // with one wave on a SIMD; 5.6 with two); products at a higher wave priority (5.4); V
 // converted and paired between the products (5.1).

@@ -56,7 +56,11 @@ constexpr int kv4_tile(int i, int row_tiles, int runs) {
 constexpr int kv4_split_at(int n, int split, int n_split) { return (int)((uint32_t)n * (uint32_t)split / (uint32_t)n_split); }
 
 // Time of a call in ns with q row tiles a workgroup (of `tiles` such tiles) and s
-// workgroups over the keys of each, from measurements on a chip with 256 CUs:
+// workgroups over the keys of each, from measurements on a chip with 256 CUs, of kernels that
+// held the softmax weights as one bf16 number (the second one adds up to 10% with one and two row
+// tiles, and a third to a call of four that writes fp32).  head_dim 64 is not modelled apart: of its kernels
+// with one and two row tiles 5 and 4 workgroups fit on a CU, not 4 and 2, and its steps take other times;
+// the factor 0.85 stands for all of that.
 //  * what a workgroup needs besides its steps: 4.3, 5.5 and 8 us for 1, 2 and 4 row tiles;
 //  * a wave's steps one after the other, 630, 650 and 1080 ns each while a CU has one
 //    workgroup, 400, 600 and 830 ns a workgroup where its instructions are the limit

@@ -3,8 +3,9 @@
 //
 // Pair p of a token turns by theta = position * inv_freq[p].  The angle is taken in
 // quarter turns in fp64, t = position * (inv_freq[p] * 2 / pi): its nearest integer
-// gives the quadrant, the rest r in [-1/2, 1/2] goes to fp32, so far positions keep
-// an absolute angle error below 1e-7 + position * 2e-16 radians.  sin and cos of
+// gives the quadrant, the rest r in [-1/2, 1/2] goes to fp32, so far positions keep an
+// absolute angle error below 1e-7 + 3.4e-16 * |position * inv_freq[p]| radians (three
+// roundings in fp64, of 2^-53 each).  sin and cos of
 // r * pi / 2 are their Taylor sums (to r^9 and r^10: the first terms left out are
 // below 2e-9 and 5e-10).
 //
@@ -184,7 +185,8 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(const RopeParams p) {
 // elements): a thread turns the E elements of its own unit, and takes their partners, at any
 // place of the row, from LDS.  A block's rows are whole heads, and all of them are read
 // before the first is written, so y may be x here too.  90 of 128 elements turned, 65280 tokens of
-// 12 heads (401 MB): 81 us, 4.9 TB/s (205 us with one pair a thread).
+// 12 heads (401 MB): 82 to 92 us, 4.4 to 4.9 TB/s, with vector instructions issuing in 86% of
+// the cycles: each sine is taken twice (205 us with one pair a thread).
 template <bool X32, bool Y32, int HEADS, int D>
 __global__ __launch_bounds__(kThreads) void rope_ragged_kernel(const RopeParams p) {
   constexpr int E = kUnit<X32, Y32>, kUnits = D / E;
